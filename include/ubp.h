@@ -228,6 +228,41 @@ ubp_status ubp_spmm_fused(const ubp_packed *p, const void *X_dev, int64_t ldx, i
                           void *Y_dev, int64_t ldy, ubp_dtype y_dtype, const ubp_epilogue *epilogue,
                           void *hip_stream, const ubp_plan *plan);
 
+/* Activations of a layer. */
+enum {
+    UBP_ACT_NONE = 0,
+    UBP_ACT_RELU = 1,      /* max(v, 0)                                                        */
+    UBP_ACT_CLAMP = 2,     /* v to [lo, hi]                                                    */
+    UBP_ACT_GELU = 3,      /* v Phi(v), Phi the normal distribution (the erf form)             */
+    UBP_ACT_GELU_TANH = 4, /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2                */
+    UBP_ACT_SILU = 5       /* v / (1 + exp(-v))                                                */
+};
+
+/*
+ * A pruned linear layer in one call, with the activations and the residual of a transformer's layers:
+ *     Y[i][j] = act( sum_k W[i][k] X[k][j] + bias[i] ) + residual[i][j],
+ * all in fp32 before the one rounding to y_dtype.  Everything else about the call - kernels, choice, allocation, Inf and NaN in
+ * X - is as for ubp_spmm_fused; ubp_spmm_prepare with the same arguments prepares it.
+ *   bias_dev     : as in ubp_epilogue.
+ *   activation   : UBP_ACT_*; UBP_ACT_CLAMP requires lo <= hi.  ReLU and clamp turn a NaN into the lower bound; with the
+ *                  others a NaN stays one, and v = -Inf gives NaN.
+ *   residual_dev : DEVICE pointer to an M x N matrix of y_dtype, leading dimension ldr (elements, >= N; any alignment), or
+ *                  NULL.  It must not share memory with Y, which is checked (UBP_ERR_INVALID_ARG): a layer adds to a
+ *                  residual stream by writing the next one.  It may lie beside Y in rows of one pitch.
+ * plan->kernel 3 with a residual or with one of the last three activations returns UBP_ERR_UNSUPPORTED.
+ * epilogue == NULL is ubp_spmm / ubp_spmm_plan; plan may be NULL.
+ */
+typedef struct {
+    const float *bias_dev;
+    const void *residual_dev;
+    int64_t ldr;
+    int32_t activation;
+    float lo, hi;
+} ubp_linear_epilogue;
+
+ubp_status ubp_linear(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t N, void *Y_dev, int64_t ldy,
+                      ubp_dtype y_dtype, const ubp_linear_epilogue *epilogue, void *hip_stream, const ubp_plan *plan);
+
 /*
  * Everything ubp_spmm_plan does with these arguments except the launch: resolves the kernel
  * and its shape, builds and uploads the re-layout of W that shape reads (host and device

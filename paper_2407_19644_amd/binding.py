@@ -26,8 +26,8 @@ EXPORTS = ("ubp_target_block_count", "ubp_select_reference", "ubp_pack", "ubp_pa
            "ubp_packed_free", "ubp_status_string", "ubp_packed_device_error", "ubp_packed_layout",
            "ubp_spmm_prepare", "ubp_launch_floor", "ubp_block_scores", "ubp_select_greedy", "ubp_select_bed",
            "ubp_select_optimal", "ubp_selection_to_blocks", "ubp_select_blocks", "ubp_selection_efficacy",
-           "ubp_spmm_fused")
-ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "clamp": 2}
+           "ubp_spmm_fused", "ubp_linear")
+ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "clamp": 2, "gelu": 3, "gelu_tanh": 4, "silu": 5}
 SELECT_METHODS = {"greedy": 0, "bed": 1, "optimal": 2}
 
 
@@ -47,6 +47,12 @@ class Plan(ctypes.Structure):
 class Epilogue(ctypes.Structure):
     """Mirror of ubp_epilogue."""
     _fields_ = [("bias_dev", ctypes.c_void_p), ("activation", ctypes.c_int32), ("lo", ctypes.c_float), ("hi", ctypes.c_float)]
+
+
+class LinearEpilogue(ctypes.Structure):
+    """Mirror of ubp_linear_epilogue."""
+    _fields_ = [("bias_dev", ctypes.c_void_p), ("residual_dev", ctypes.c_void_p), ("ldr", ctypes.c_int64),
+                ("activation", ctypes.c_int32), ("lo", ctypes.c_float), ("hi", ctypes.c_float)]
 
 
 _lib = None
@@ -90,6 +96,8 @@ def load_library():
     L.ubp_spmm_prepare.restype = ctypes.c_int
     L.ubp_spmm_fused.argtypes = [vp, vp, i64, i32, vp, i64, ctypes.c_int, ctypes.POINTER(Epilogue), vp, ctypes.POINTER(Plan)]
     L.ubp_spmm_fused.restype = ctypes.c_int
+    L.ubp_linear.argtypes = [vp, vp, i64, i32, vp, i64, ctypes.c_int, ctypes.POINTER(LinearEpilogue), vp, ctypes.POINTER(Plan)]
+    L.ubp_linear.restype = ctypes.c_int
     L.ubp_launch_floor.argtypes = [vp]
     L.ubp_launch_floor.restype = ctypes.c_int
     L.ubp_block_scores.argtypes = [vp, ctypes.c_int, i64, i32, i32, i32, i32, i32, vp, i64]
@@ -335,12 +343,23 @@ def spmm(packed, X_ptr, ldx, N, Y_ptr, ldy, y_dtype, stream=0, plan=None):
 def spmm_fused(packed, X_ptr, ldx, N, Y_ptr, ldy, y_dtype, bias_ptr=None, activation=None, lo=0.0, hi=0.0, stream=0,
                plan=None):
     """ubp_spmm_fused with raw DEVICE pointers; bias_ptr: M floats on the device or None;
-    activation: None / "relu" / "clamp" (with lo, hi)."""
+    activation: None / "relu" / "clamp" (with lo, hi); linear() takes the others too."""
     ep = Epilogue(bias_ptr, ACTIVATIONS[activation], float(lo), float(hi))
     rc = load_library().ubp_spmm_fused(packed.handle, X_ptr, ldx, N, Y_ptr, ldy, DTYPES[y_dtype], ctypes.byref(ep), stream,
                                        ctypes.byref(plan) if plan is not None else None)
     if rc != UBP_OK:
         raise UBPError(rc, "ubp_spmm_fused")
+
+
+def linear(packed, X_ptr, ldx, N, Y_ptr, ldy, y_dtype, bias_ptr=None, activation=None, lo=0.0, hi=0.0, residual_ptr=None,
+           ldr=0, stream=0, plan=None):
+    """ubp_linear with raw DEVICE pointers: Y = act(W X + bias) + residual.  activation: a key of ACTIVATIONS; residual_ptr:
+    M x N of Y's type with pitch ldr, or None."""
+    ep = LinearEpilogue(bias_ptr, residual_ptr, ldr, ACTIVATIONS[activation], float(lo), float(hi))
+    rc = load_library().ubp_linear(packed.handle, X_ptr, ldx, N, Y_ptr, ldy, DTYPES[y_dtype], ctypes.byref(ep), stream,
+                                   ctypes.byref(plan) if plan is not None else None)
+    if rc != UBP_OK:
+        raise UBPError(rc, "ubp_linear")
 
 
 def spmm_prepare(packed, X_ptr, ldx, N, Y_ptr, ldy, y_dtype, plan=None):

@@ -12,7 +12,11 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libubp.so")
 HOST_SOURCES = ["ubp_host.cpp", "ubp_layouts.cpp", "ubp_choose.cpp", "ubp_select.cpp"]
 HIP_SOURCES = ["ubp_api.hip", "ubp_wros.hip", "ubp_wros4.hip", "ubp_stripe.hip", "ubp_blk.hip", "ubp_tile.hip", "ubp_direct.hip", "ubp_mtile.hip"]
+# compiled a second time with UBP_WIDE: the epilogue with activations beyond a clamp and a residual
+WIDE_SOURCES = ["ubp_wros.hip", "ubp_wros4.hip", "ubp_stripe.hip", "ubp_blk.hip", "ubp_tile.hip", "ubp_direct.hip", "ubp_mtile.hip"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result"]
+# sources that take longest to compile come first
+LONG = ("ubp_wros", "ubp_mtile", "ubp_stripe", "ubp_wros4")
 # packed-fp32 VALU forms are switched off for every device function in this library
 HIP_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
@@ -31,6 +35,11 @@ def build_library(verbose=False, jobs=None, defines=(), out=None):
         for s in HIP_SOURCES:
             obj = os.path.join(tmpdir, s + ".o")
             cmds.append((obj, [hipcc] + COMMON + HIP_FLAGS + inc + ["-x", "hip", "-c", os.path.join(CSRC, s), "-o", obj]))
+
+        for s in WIDE_SOURCES:
+            obj = os.path.join(tmpdir, s + ".wide.o")
+            cmds.append((obj, [hipcc] + COMMON + HIP_FLAGS + inc + ["-DUBP_WIDE", "-x", "hip", "-c", os.path.join(CSRC, s), "-o", obj]))
+        cmds.sort(key=lambda c: os.path.basename(c[0]).split(".")[0] not in LONG)
 
         def run(item):
             obj, cmd = item

@@ -264,23 +264,60 @@ StripeArgs stripe_args(const ubp_packed *p, const Shape &s, const void *X, int64
     return a;
 }
 
-// The whole of ubp_spmm_plan / ubp_spmm_prepare.  dry: everything but the launch.
+// What a caller asks for between the accumulator and the store, in the kernels' form.
+ubp_status epilogue_of(const ubp_linear_epilogue *fused, Epilogue &ep) {
+    if (!fused) return UBP_OK;
+    const int act = fused->activation;
+    if (act < UBP_ACT_NONE || act > UBP_ACT_SILU) return UBP_ERR_INVALID_ARG;
+    if (act == UBP_ACT_CLAMP && !(fused->lo <= fused->hi)) return UBP_ERR_INVALID_ARG; // (also refuses NaN bounds)
+    ep.bias = fused->bias_dev;
+    ep.res = fused->residual_dev;
+    ep.ldr = fused->ldr;
+    ep.on = (ep.res != nullptr || act > UBP_ACT_CLAMP) ? 2 : (ep.bias != nullptr || act != UBP_ACT_NONE) ? 1 : 0;
+    ep.lo = act == UBP_ACT_RELU ? 0.f : act == UBP_ACT_CLAMP ? fused->lo : -INFINITY;
+    ep.hi = act == UBP_ACT_CLAMP ? fused->hi : INFINITY;
+    activation_of(act, ep.act, ep.c1, ep.c3);
+    return UBP_OK;
+}
+
+// Whether rows of `a` and of `b` share memory: M rows of N elements of `size` bytes each.  Rows side by side in rows of one
+// pitch (two column ranges of one matrix) do not.
+bool rows_overlap(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t size) {
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+    const unsigned __int128 a1 = (unsigned __int128)a0 + (unsigned __int128)((M - 1) * (__int128)lda + N) * size;
+    const unsigned __int128 b1 = (unsigned __int128)b0 + (unsigned __int128)((M - 1) * (__int128)ldb + N) * size;
+    if (a0 >= b1 || b0 >= a1) return false;
+    if (M == 1 || lda != ldb) return true;
+    const uint64_t pitch = (uint64_t)lda * (uint64_t)size, row = (uint64_t)N * (uint64_t)size;
+    const uint64_t apart = (a0 > b0 ? a0 - b0 : b0 - a0) % pitch;
+    return apart < row || pitch - apart < row;
+}
+
+// One launch through the kernels with the plain or with the wide epilogue; a preparation goes through both.
+template <class Plain, class Wide, class... A>
+ubp_status launch_either(Plain plain, Wide wide, const Epilogue &ep, bool dry, const A &...a) {
+    if (!dry) return ep.on == 2 ? wide(a..., dry) : plain(a..., dry);
+    const ubp_status rc = plain(a..., dry);
+    if (rc == UBP_OK) (void)wide(a..., dry);
+    return rc;
+}
+
+// The whole of ubp_spmm_plan / ubp_spmm_prepare / ubp_linear.  dry: everything but the launch.
 ubp_status execute(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t N, void *Y_dev, int64_t ldy, ubp_dtype y_dtype,
-                   void *stream, const ubp_plan *plan, bool dry, ubp_plan *chosen, const ubp_epilogue *fused) try {
+                   void *stream, const ubp_plan *plan, bool dry, ubp_plan *chosen, const ubp_linear_epilogue *fused) try {
     if (!p || N < 0) return UBP_ERR_INVALID_ARG;
-    Epilogue ep = {nullptr, 0, 0.f, 0.f};
-    if (fused) {
-        if (fused->activation < 0 || fused->activation > 2) return UBP_ERR_INVALID_ARG;
-        if (fused->activation == 2 && !(fused->lo <= fused->hi)) return UBP_ERR_INVALID_ARG; // (also refuses NaN bounds)
-        ep.bias = fused->bias_dev;
-        ep.on = (fused->bias_dev != nullptr || fused->activation != 0) ? 1 : 0;
-        ep.lo = fused->activation == 1 ? 0.f : fused->activation == 2 ? fused->lo : -INFINITY;
-        ep.hi = fused->activation == 2 ? fused->hi : INFINITY;
-    }
+    Epilogue ep = {};
+    const ubp_status bad = epilogue_of(fused, ep);
+    if (bad != UBP_OK) return bad;
     if (p->device == UBP_HOST_ONLY) return UBP_ERR_INVALID_ARG;
     if (y_dtype != UBP_F32 && y_dtype != p->dtype) return UBP_ERR_INVALID_ARG;
     if (N == 0) return UBP_OK;
     if (!X_dev || !Y_dev || ldx < N || ldy < N) return UBP_ERR_INVALID_ARG;
+    if (ep.res) {
+        // (a pixel that two workgroups compute would find its residual overwritten)
+        if (ep.ldr < N || rows_overlap(ep.res, ep.ldr, Y_dev, ldy, p->M, N, y_dtype == UBP_F32 ? 4 : 2)) return UBP_ERR_INVALID_ARG;
+        ep.res_vec = (ep.ldr * (y_dtype == UBP_F32 ? 4 : 2)) % 16 == 0 && reinterpret_cast<uintptr_t>(ep.res) % 16 == 0;
+    }
     ubp_plan pl;
     std::memset(&pl, 0, sizeof pl);
     if (plan) pl = *plan;
@@ -373,11 +410,13 @@ ubp_status execute(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t 
             a.slices = (int)(((int64_t)p->M + (int64_t)s.rpr * s.px_waves - 1) / ((int64_t)s.rpr * s.px_waves));
             a.vec4 = (N % 4 == 0) && (ldx % 4 == 0) && (reinterpret_cast<uintptr_t>(X_dev) % 16 == 0);
             a.ep = ep;
-            return launch_wros4(a, p->bh, s.px, s.px_waves, stream, dry);
+            return launch_either(launch_wros4, launch_wros4_wide, ep, dry, a, p->bh, s.px, s.px_waves, stream);
         }
         [[fallthrough]];
-    case 3: return launch_wros(p, X_dev, ldx, N, Y_dev, ldy, y_dtype, s.rpr, s.kernel == 3, ep, stream, dry);
-    case 2: return launch_stripe(stripe_args(p, s, X_dev, ldx, N, Y_dev, ldy, vec_ok, 0, ep), bf16, y_f32, s.G, s.CT, s.waves, stream, dry);
+    case 3: return launch_either(launch_wros, launch_wros_wide, ep, dry, p, X_dev, ldx, N, Y_dev, ldy, y_dtype, s.rpr, s.kernel == 3, ep, stream);
+    case 2:
+        return launch_either(launch_stripe, launch_stripe_wide, ep, dry, stripe_args(p, s, X_dev, ldx, N, Y_dev, ldy, vec_ok, 0, ep),
+                             bf16, y_f32, s.G, s.CT, s.waves, stream);
     case 4:
     case 5:
     case 9:
@@ -401,8 +440,8 @@ ubp_status execute(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t 
         a.n_blocks = (N + 16 * s.CT - 1) / (16 * s.CT); // (kernel 4; the others count their own tiles)
         a.slices = s.wg_rows;
         a.sps = (T.nstripes + s.wg_rows - 1) / s.wg_rows;
-        if (s.kernel == 4) return launch_xstat(a, bf16, y_f32, s.CT, T.kt_pad, s.waves, stream, dry);
-        return launch_mtile(a, bf16, y_f32, s.shape, s.rows, stream, dry);
+        if (s.kernel == 4) return launch_either(launch_xstat, launch_xstat_wide, ep, dry, a, bf16, y_f32, s.CT, T.kt_pad, s.waves, stream);
+        return launch_either(launch_mtile, launch_mtile_wide, ep, dry, a, bf16, y_f32, s.shape, s.rows, stream);
     }
     case 8: {
         DirectArgs a = {};
@@ -418,7 +457,7 @@ ubp_status execute(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t 
         a.N = N;
         a.nstripes = p->direct.nstripes;
         a.ep = ep;
-        return launch_direct(a, bf16, y_f32, s.CT, s.waves, stream, dry);
+        return launch_either(launch_direct, launch_direct_wide, ep, dry, a, bf16, y_f32, s.CT, s.waves, stream);
     }
     case 6: {
         const int slot = blk_slot(s.G);
@@ -447,10 +486,10 @@ ubp_status execute(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t 
         a.out_bytes = 0; // set per launch
         a.err = p->d_error;
         a.ep = ep;
-        ubp_status rc = launch_blk(a, bf16, y_f32, s.G, s.waves, stream, dry);
+        ubp_status rc = launch_either(launch_blk, launch_blk_wide, ep, dry, a, bf16, y_f32, s.G, s.waves, stream);
         if (rc == UBP_OK && has_tail)
-            rc = launch_stripe(stripe_args(p, tail, X_dev, ldx, N, Y_dev, ldy, vec_ok, N / 64, ep), bf16, y_f32, tail.G, tail.CT,
-                               tail.waves, stream, dry);
+            rc = launch_either(launch_stripe, launch_stripe_wide, ep, dry, stripe_args(p, tail, X_dev, ldx, N, Y_dev, ldy, vec_ok, N / 64, ep),
+                               bf16, y_f32, tail.G, tail.CT, tail.waves, stream);
         return rc;
     }
     }
@@ -480,6 +519,19 @@ ubp_status ubp_spmm(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t
 
 ubp_status ubp_spmm_fused(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t N, void *Y_dev, int64_t ldy,
                           ubp_dtype y_dtype, const ubp_epilogue *epilogue, void *hip_stream, const ubp_plan *plan) {
+    ubp_linear_epilogue e = {};
+    if (epilogue) {
+        if (epilogue->activation < UBP_ACT_NONE || epilogue->activation > UBP_ACT_CLAMP) return UBP_ERR_INVALID_ARG;
+        e.bias_dev = epilogue->bias_dev;
+        e.activation = epilogue->activation;
+        e.lo = epilogue->lo;
+        e.hi = epilogue->hi;
+    }
+    return ubp::execute(p, X_dev, ldx, N, Y_dev, ldy, y_dtype, hip_stream, plan, false, nullptr, &e);
+}
+
+ubp_status ubp_linear(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t N, void *Y_dev, int64_t ldy,
+                      ubp_dtype y_dtype, const ubp_linear_epilogue *epilogue, void *hip_stream, const ubp_plan *plan) {
     return ubp::execute(p, X_dev, ldx, N, Y_dev, ldy, y_dtype, hip_stream, plan, false, nullptr, epilogue);
 }
 

@@ -384,8 +384,17 @@ __global__ __launch_bounds__(MAXT) void blk_kernel(BlkArgs a) {
     // ---- store: lane (g = lane/16, n = lane%16) holds pixels col0 + 16*c + 4*g + v of row
     // 16*(stripe0 + j) + n, j < stripes.  Rows no block touches are stored as zeros like any other.
     TY *Yt = static_cast<TY *>(a.Y);
-    // the epilogue (bias of the lane's row, clamp) is applied tile by tile on the way out
-    const bool fused = a.ep.on != 0;
+    // the epilogue (bias of the lane's row, activation, residual) is applied tile by tile on the way out; a stripe's
+    // residual is asked for before the stripe before it leaves
+    const bool fused = kWide || a.ep.on != 0;
+    [[maybe_unused]] Residual<TY, 4> res[CT];
+    [[maybe_unused]] auto load_residual = [&](int j) {
+        int row = j < stripes ? (stripe0 + j) * kStripe + n : a.M;
+        asm volatile("" : "+v"(row)); // (or the addresses of all stripes are worked out first, and spilled)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) res[c].load(a.ep, row, col0 + 16 * c + 4 * g, a.M, a.N);
+    };
+    if constexpr (kWide) load_residual(0);
     if constexpr (sizeof(TY) == 2) {
         if (a.out_bytes != 0) {
             // A 16-bit tile straight from the accumulators is 8 bytes per lane, 32-byte runs per
@@ -405,12 +414,15 @@ __global__ __launch_bounds__(MAXT) void blk_kernel(BlkArgs a) {
                 for (int c = 0; c < CT; ++c) {
                     typedef TY ty4 __attribute__((ext_vector_type(4)));
                     ty4 o;
-                    if (fused) epilogue_tile(a.ep, acc[j][c], bj);
+                    if constexpr (kWide) res[c].apply(a.ep, acc[j][c], bj);
+                    else if (fused) epilogue_tile(a.ep, acc[j][c], bj);
 #pragma unroll
                     for (int v = 0; v < 4; ++v) o[v] = from_f32<TY>(acc[j][c][v]);
                     const int piece = (2 * c + (g >> 1)) ^ ((n / RP) & (PR - 1));
                     *reinterpret_cast<ty4 *>(scratch + n * RB + piece * 16 + (g & 1) * 8) = o;
                 }
+                if constexpr (kWide)
+                    if (j + 1 < G) load_residual(j + 1);
 #pragma unroll
                 for (int i = 0; i < NI; ++i) {
                     const int r = i * (64 / PR) + lane / PR, lp = lane % PR;
@@ -431,10 +443,13 @@ __global__ __launch_bounds__(MAXT) void blk_kernel(BlkArgs a) {
         for (int c = 0; c < CT; ++c) {
             const int px = col0 + 16 * c + 4 * g;
             TY *dst = Yt + (int64_t)row * a.ldy + px;
-            if (fused) epilogue_tile(a.ep, acc[j][c], bj);
+            if constexpr (kWide) res[c].apply(a.ep, acc[j][c], bj);
+            else if (fused) epilogue_tile(a.ep, acc[j][c], bj);
             float v[4] = {acc[j][c][0], acc[j][c][1], acc[j][c][2], acc[j][c][3]};
             store_row<TY, 4>(dst, v);
         }
+        if constexpr (kWide)
+            if (j + 1 < G) load_residual(j + 1);
     }
 }
 
@@ -464,7 +479,7 @@ ubp_status launch_blk_t(const BlkArgs &a, int G, int waves, hipStream_t st, bool
 
 } // namespace
 
-ubp_status launch_blk(const BlkArgs &a, bool bf16, bool y_f32, int G, int waves, void *stream, bool dry) {
+ubp_status UBP_LAUNCHER(launch_blk)(const BlkArgs &a, bool bf16, bool y_f32, int G, int waves, void *stream, bool dry) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     // 64 rows of ldx elements must fit the producer's 32-bit lane offsets
     if (a.ldx > (int64_t(1) << 24)) return UBP_ERR_UNSUPPORTED;

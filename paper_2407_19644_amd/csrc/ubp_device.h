@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cstdint>
+#include <type_traits>
 
 #include "ubp_internal.h"
 
@@ -62,6 +63,107 @@ __device__ __forceinline__ void epilogue_tile(const Epilogue &e, float4v &acc, f
 #pragma unroll
     for (int v = 0; v < 4; ++v) acc[v] = epilogue_value(e, acc[v], b);
 }
+
+// ---- activations beyond a clamp.  Both are v times a distribution function of v, so that one quotient or one polynomial
+// gives the function and, in the backward pass, its slope.
+// sigma(u) by the hardware's exp2 and reciprocal (1 ulp each); u so large that exp2 overflows gives 0.
+__device__ __forceinline__ float sigmoid(float u) {
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * -1.44269504089f));
+}
+// Phi(v) = 1/2 erfc(-v / sqrt 2).  The tail Q(z) = 1 - Phi(z), z >= 0, is exp(-z^2 / 2) times a smooth function, here a
+// polynomial in t = 1 / (1 + 0.3 z): fitted for the smallest largest relative error on 0 <= z <= 14.5, where Q leaves
+// fp32, 5e-8; in fp32 Phi is within 2e-7 of the truth and its tail within 1.4e-6 of itself up to z = 5 (the rounding of z^2).
+// density: exp(-v^2 / 2), which the slope needs too.
+__device__ __forceinline__ float normal_cdf(float v, float &density) {
+    const float z = fabsf(v), t = __builtin_amdgcn_rcpf(fmaf(0.3f, z, 1.f));
+    density = __builtin_amdgcn_exp2f(z * z * -0.72134752044f);
+    float q = 0.03831019252538681f;
+    q = fmaf(q, t, -0.168900728225708f);
+    q = fmaf(q, t, 0.22824111580848694f);
+    q = fmaf(q, t, -0.07616594433784485f);
+    q = fmaf(q, t, 0.14238862693309784f);
+    q = fmaf(q, t, 0.09471195936203003f);
+    q = fmaf(q, t, 0.12192083895206451f);
+    q = fmaf(q, t, 0.11948668211698532f);
+    q = fmaf(q, t, 7.272966286109295e-06f) * density;
+    return v > 0.f ? 1.f - q : q;
+}
+// The argument of the odd polynomial c1 v + c3 v^3, kept where its powers are finite: sigma is 0 or 1 long before.
+__device__ __forceinline__ float cubic(float v, float c1, float c3) {
+    const float w = fminf(fmaxf(v, -1e9f), 1e9f);
+    return w * fmaf(c3 * w, w, c1);
+}
+
+// The kernels' sources are compiled twice: as they are, and with UBP_WIDE for the epilogue with on == 2, whose activations
+// and residual take registers that the plain kernels have better use for (in one kernel behind a branch, the block kernel
+// spilled 120 registers and 50 others lost a wavefront per SIMD).  The launchers of the second kind have names of their own.
+#ifdef UBP_WIDE
+constexpr bool kWide = true;
+#define UBP_LAUNCHER(name) name##_wide
+#else
+constexpr bool kWide = false;
+#define UBP_LAUNCHER(name) name
+#endif
+
+// Epilogue with on == 2, without the residual.
+__device__ __forceinline__ void epilogue_act(const Epilogue &e, float *v, int n, float b) {
+    if (e.act == kActSigmoid) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float x = v[i] + b;
+            v[i] = x * sigmoid(cubic(x, e.c1, e.c3));
+        }
+    } else if (e.act == kActNormal) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float x = v[i] + b;
+            float d;
+            v[i] = x * normal_cdf(x, d);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = epilogue_value(e, v[i], b);
+    }
+}
+// n neighbouring values of the residual (pixels px .. of a row; nothing outside the M x N matrix is read; zeros without one).
+template <typename TY, int VEC> struct Residual {
+    typedef typename std::conditional<sizeof(TY) == 4, uint32_t, uint16_t>::type Bits;
+    static constexpr int kWords = (VEC * (int)sizeof(TY) + 3) / 4;
+    uint32_t r[kWords]; // (packed: the wavefronts that hold these have few registers left)
+    __device__ __forceinline__ void load(const Epilogue &e, int row, int px, int M, int N) {
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) r[w] = 0u;
+        if (e.res == nullptr || row >= M) return;
+        const Bits *src = static_cast<const Bits *>(e.res) + (int64_t)row * e.ldr + px;
+        if (VEC > 1 && e.res_vec && px + VEC <= N) {
+            typedef typename VecOf<Bits, VEC>::type V;
+            const V x = *reinterpret_cast<const V *>(src);
+            __builtin_memcpy(r, &x, sizeof x);
+        } else {
+#pragma unroll
+            for (int v = 0; v < VEC; ++v)
+                if (px + v < N) {
+                    if constexpr (sizeof(TY) == 4) r[v] = src[v];
+                    else r[v / 2] |= (uint32_t)src[v] << (16 * (v & 1));
+                }
+        }
+    }
+    __device__ __forceinline__ float value(int v) const {
+        if constexpr (sizeof(TY) == 4) return __builtin_bit_cast(float, r[v]);
+        else return to_f32(__builtin_bit_cast(TY, (uint16_t)(r[v / 2] >> (16 * (v & 1)))));
+    }
+    // act(v + b) + residual
+    __device__ __forceinline__ void apply(const Epilogue &e, float (&v)[VEC], float b) const {
+        epilogue_act(e, v, VEC, b);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] += value(i);
+    }
+    __device__ __forceinline__ void apply(const Epilogue &e, float4v &acc, float b) const {
+        float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+        apply(e, v, b);
+        acc = float4v{v[0], v[1], v[2], v[3]};
+    }
+};
 
 template <bool BF16>
 __device__ __forceinline__ float4v mfma16(short8v a, short8v b, float4v c) {

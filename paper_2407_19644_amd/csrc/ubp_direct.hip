@@ -111,15 +111,23 @@ __global__ __launch_bounds__(1024) void direct_kernel(DirectArgs a) {
         }
     }
 
-    // ---- sums over the wavefronts, epilogue, store: wavefront v mod NW takes rows 4 g + v
+    // ---- sums over the wavefronts, epilogue, store: wavefront v mod NW takes rows 4 g + v.  The residual of the
+    // first of them is asked for before the sums meet.
+    [[maybe_unused]] Residual<TY, CT> res;
+    [[maybe_unused]] auto load_residual = [&](int v) { res.load(a.ep, stripe * kStripe + 4 * g + v, col, a.M, a.N); };
+    if constexpr (kWide) load_residual(NW == 1 ? 0 : wave < 4 ? wave : 0);
     TY *Yt = static_cast<TY *>(a.Y);
     auto put = [&](int v, float(&o)[CT]) {
         const int row = stripe * kStripe + 4 * g + v;
         if (row >= a.M) return;
         if (a.ep.on) {
             const float b = epilogue_bias(a.ep, row, a.M);
+            if constexpr (kWide) {
+                res.apply(a.ep, o, b);
+            } else {
 #pragma unroll
-            for (int t = 0; t < CT; ++t) o[t] = epilogue_value(a.ep, o[t], b);
+                for (int t = 0; t < CT; ++t) o[t] = epilogue_value(a.ep, o[t], b);
+            }
         }
         TY r[CT];
 #pragma unroll
@@ -139,6 +147,7 @@ __global__ __launch_bounds__(1024) void direct_kernel(DirectArgs a) {
             float o[CT];
 #pragma unroll
             for (int t = 0; t < CT; ++t) o[t] = acc[t][v];
+            if constexpr (kWide) if (v != 0) load_residual(v);
             put(v, o);
         }
         return;
@@ -153,6 +162,7 @@ __global__ __launch_bounds__(1024) void direct_kernel(DirectArgs a) {
         float o[CT];
 #pragma unroll
         for (int t = 0; t < CT; ++t) o[t] = part[(t * 4 + v) * 64 + lane];
+        if constexpr (kWide) if (v != wave) load_residual(v);
         for (int w = 1; w < NW; ++w)
 #pragma unroll
             for (int t = 0; t < CT; ++t) o[t] += part[((w * CT + t) * 4 + v) * 64 + lane];
@@ -180,7 +190,7 @@ ubp_status launch_direct_t(const DirectArgs &a, int CT, int waves, hipStream_t s
 
 } // namespace
 
-ubp_status launch_direct(const DirectArgs &a, bool bf16, bool y_f32, int CT, int waves, void *stream, bool dry) {
+ubp_status UBP_LAUNCHER(launch_direct)(const DirectArgs &a, bool bf16, bool y_f32, int CT, int waves, void *stream, bool dry) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (bf16) return y_f32 ? launch_direct_t<true, float>(a, CT, waves, st, dry) : launch_direct_t<true, __bf16>(a, CT, waves, st, dry);
     return y_f32 ? launch_direct_t<false, float>(a, CT, waves, st, dry) : launch_direct_t<false, _Float16>(a, CT, waves, st, dry);

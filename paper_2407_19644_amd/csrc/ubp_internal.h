@@ -247,14 +247,28 @@ struct TileLayoutDev {
 };
 
 // ------------------------------------------------------------------ kernel arguments
-// What happens to an output value between the accumulator and the store: Y = act(acc + bias[row]),
-// in fp32, before the one rounding to Y's type.  on == 0: nothing.  The activation is a clamp to
-// [lo, hi] (ReLU: lo = 0, hi = +inf), taken with maxNum / minNum, so that a NaN becomes lo.
+// What happens to an output value between the accumulator and the store: Y = act(acc + bias[row]) + res[row][pixel],
+// in fp32, before the one rounding to Y's type.  on == 0: nothing.  on == 1: no residual, and the activation is a clamp to
+// [lo, hi] (ReLU: lo = 0, hi = +inf), taken with maxNum / minNum, so that a NaN becomes lo.  on == 2: the activation is
+// `act`, and res, where there is one, is added.
+enum : int { kActClamp = 0, kActSigmoid = 1, kActNormal = 2 };
 struct Epilogue {
     const float *bias; // device, M floats, or null
     int on;
     float lo, hi;
+    int act;           // kActClamp; kActSigmoid: v sigma(c1 v + c3 v^3); kActNormal: v Phi(v), Phi the normal distribution
+    float c1, c3;
+    const void *res;   // device, M rows of Y's type, or null
+    int64_t ldr;
+    int res_vec;       // rows of res start at multiples of 16 bytes
 };
+
+inline void activation_of(int activation, int &act, float &c1, float &c3) {
+    act = activation == UBP_ACT_GELU ? kActNormal : activation > UBP_ACT_GELU ? kActSigmoid : kActClamp;
+    // (1 + tanh u) / 2 = sigma(2 u)
+    c1 = activation == UBP_ACT_GELU_TANH ? 1.5957691216f : 1.f;
+    c3 = activation == UBP_ACT_GELU_TANH ? 0.071354816272f : 0.f;
+}
 
 struct StripeArgs {
     const int32_t *rg_ptr;
@@ -446,5 +460,14 @@ constexpr int kNumMtileShapes = 5;
 constexpr MtileShape kMtileShapes[kNumMtileShapes] = {{128, 128, 1}, {128, 64, 1}, {64, 128, 1}, {64, 64, 2}, {128, 256, 1}};
 ubp_status launch_mtile(const TileArgs &a, bool bf16, bool y_f32, int shape, int rows, void *stream, bool dry);
 ubp_status launch_floor(void *stream);
+// The same kernels with the epilogue of ep.on == 2 (the sources compiled with UBP_WIDE).
+ubp_status launch_wros_wide(const ubp_packed *p, const void *X, int64_t ldx, int N, void *Y, int64_t ldy, ubp_dtype y_dtype,
+                            int rpr, bool naive, const Epilogue &ep, void *stream, bool dry);
+ubp_status launch_wros4_wide(const Wros4Args &a, int bh, int PX, int waves, void *stream, bool dry);
+ubp_status launch_stripe_wide(const StripeArgs &a, bool bf16, bool y_f32, int G, int CT, int waves, void *stream, bool dry);
+ubp_status launch_blk_wide(const BlkArgs &a, bool bf16, bool y_f32, int G, int waves, void *stream, bool dry);
+ubp_status launch_xstat_wide(const TileArgs &a, bool bf16, bool y_f32, int CT, int KT, int waves, void *stream, bool dry);
+ubp_status launch_direct_wide(const DirectArgs &a, bool bf16, bool y_f32, int CT, int waves, void *stream, bool dry);
+ubp_status launch_mtile_wide(const TileArgs &a, bool bf16, bool y_f32, int shape, int rows, void *stream, bool dry);
 
 } // namespace ubp

@@ -335,7 +335,14 @@ __global__ __launch_bounds__((WM * WN + NPW) * 64, 2) void mtile_kernel(TileArgs
 #pragma unroll
         for (int i = 0; i < SM; ++i) {
             const int stripe = s0 + i;
-            if (a.ep.on) {
+            if constexpr (kWide) {
+                const float b = epilogue_bias(a.ep, stripe * kStripe + n, a.M);
+                Residual<TY, 4> r[PN];
+#pragma unroll
+                for (int c = 0; c < PN; ++c) r[c].load(a.ep, stripe * kStripe + n, pcol0 + 16 * c + 4 * g, a.M, a.N);
+#pragma unroll
+                for (int c = 0; c < PN; ++c) r[c].apply(a.ep, acc[i][c], b);
+            } else if (a.ep.on) {
                 const float b = epilogue_bias(a.ep, stripe * kStripe + n, a.M);
 #pragma unroll
                 for (int c = 0; c < PN; ++c) epilogue_tile(a.ep, acc[i][c], b);
@@ -434,7 +441,7 @@ ubp_status launch_t(const TileArgs &a, int shape, int rows, hipStream_t st, bool
 
 } // namespace
 
-ubp_status launch_mtile(const TileArgs &a, bool bf16, bool y_f32, int shape, int rows, void *stream, bool dry) {
+ubp_status UBP_LAUNCHER(launch_mtile)(const TileArgs &a, bool bf16, bool y_f32, int shape, int rows, void *stream, bool dry) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (bf16) return y_f32 ? launch_t<true, float>(a, shape, rows, st, dry) : launch_t<true, __bf16>(a, shape, rows, st, dry);
     return y_f32 ? launch_t<false, float>(a, shape, rows, st, dry) : launch_t<false, _Float16>(a, shape, rows, st, dry);

@@ -399,7 +399,14 @@ __global__ __launch_bounds__(stripe_max_threads(G, CT)) void stripe_kernel(Strip
         for (int j = 0; j < G; ++j) {
             const int row = (rg_done * G + j) * kStripe + n;
             if (row >= a.M) continue;
-            if (a.ep.on) {
+            if constexpr (kWide) {
+                const float b = epilogue_bias(a.ep, row, a.M);
+                Residual<TY, 4> r[CT];
+#pragma unroll
+                for (int c = 0; c < CT; ++c) r[c].load(a.ep, row, col0 + 16 * c + 4 * g, a.M, a.N);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) r[c].apply(a.ep, acc[j][c], b);
+            } else if (a.ep.on) {
                 const float b = epilogue_bias(a.ep, row, a.M);
 #pragma unroll
                 for (int c = 0; c < CT; ++c) epilogue_tile(a.ep, acc[j][c], b);
@@ -466,7 +473,7 @@ ubp_status launch_stripe_t(const StripeArgs &a, int G, int CT, int waves, hipStr
 } // namespace
 
 // a.ctile0 = first column tile this launch is responsible for (0: all of them)
-ubp_status launch_stripe(const StripeArgs &a, bool bf16, bool y_f32, int G, int CT, int waves, void *stream, bool dry) {
+ubp_status UBP_LAUNCHER(launch_stripe)(const StripeArgs &a, bool bf16, bool y_f32, int G, int CT, int waves, void *stream, bool dry) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (bf16)
         return y_f32 ? launch_stripe_t<true, float>(a, G, CT, waves, st, dry) : launch_stripe_t<true, __bf16>(a, G, CT, waves, st, dry);

@@ -179,7 +179,14 @@ __global__ __launch_bounds__(512) void xstat_kernel(TileArgs a) {
         // after the detour an instruction writes whole rows of the block (RB bytes each).
         // 16-byte pieces of a row are XOR-swizzled by the row number so that the 16 lanes LDS
         // serves together hit 64 different banks on the way in and on the way out.
-        if (a.ep.on) {
+        if constexpr (kWide) {
+            const float b = epilogue_bias(a.ep, stripe * kStripe + n, a.M);
+            Residual<TY, 4> r[CT];
+#pragma unroll
+            for (int c = 0; c < CT; ++c) r[c].load(a.ep, valid ? stripe * kStripe + n : a.M, bcol0 + PixelMap<TY>::first(c, g), a.M, a.N);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) r[c].apply(a.ep, acc[c], b);
+        } else if (a.ep.on) {
             const float b = epilogue_bias(a.ep, stripe * kStripe + n, a.M);
 #pragma unroll
             for (int c = 0; c < CT; ++c) epilogue_tile(a.ep, acc[c], b);
@@ -252,7 +259,7 @@ ubp_status launch_xstat_t(const TileArgs &a, int CT, int KT, int waves, hipStrea
 
 } // namespace
 
-ubp_status launch_xstat(const TileArgs &a, bool bf16, bool y_f32, int CT, int KT, int waves, void *stream, bool dry) {
+ubp_status UBP_LAUNCHER(launch_xstat)(const TileArgs &a, bool bf16, bool y_f32, int CT, int KT, int waves, void *stream, bool dry) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (bf16)
         return y_f32 ? launch_xstat_t<true, float>(a, CT, KT, waves, st, dry) : launch_xstat_t<true, __bf16>(a, CT, KT, waves, st, dry);

@@ -103,8 +103,14 @@ __device__ __forceinline__ void vector_walk(const int32_t *__restrict__ indptr, 
             if (i >= lo) {
                 if (ep.on) {
                     const float b = ep.bias ? ep.bias[i] : 0.f;
+                    if constexpr (kWide) {
+                        Residual<TY, VEC> r;
+                        r.load(ep, i, (int)col, M, N);
+                        r.apply(ep, acc[s], b);
+                    } else {
 #pragma unroll
-                    for (int v = 0; v < VEC; ++v) acc[s][v] = epilogue_value(ep, acc[s][v], b);
+                        for (int v = 0; v < VEC; ++v) acc[s][v] = epilogue_value(ep, acc[s][v], b);
+                    }
                 }
                 store_row<TY, VEC>(Y + (int64_t)i * ldy + col, acc[s]);
             }
@@ -137,6 +143,13 @@ __global__ __launch_bounds__(256) void naive_kernel(const int32_t *__restrict__ 
     vector_walk<TX, TY, BH, VEC, true>(indptr, cols, vals, X, ldx, Y, ldy, M, N, bw, rpr, ep);
 }
 
+// (the comparison kernel has no wide epilogue)
+template <typename TX, typename TY, int BH, int VEC> auto pick_kernel([[maybe_unused]] bool naive) {
+    if constexpr (!kWide)
+        if (naive) return &naive_kernel<TX, TY, BH, VEC>;
+    return &wros_kernel<TX, TY, BH, VEC>;
+}
+
 template <typename TX, typename TY, int VEC>
 ubp_status launch_wros_bh(const ubp_packed *p, const void *X, int64_t ldx, int N, void *Y, int64_t ldy, int rpr,
                           bool naive, const Epilogue &ep, hipStream_t st) {
@@ -145,9 +158,9 @@ ubp_status launch_wros_bh(const ubp_packed *p, const void *X, int64_t ldx, int N
     const dim3 grid((unsigned)((tiles + 7) / 8 * 8), (unsigned)((ranges + waves - 1) / waves));
 #define UBP_WROS_CASE(BH)                                                                                              \
     case BH:                                                                                                           \
-        hipLaunchKernelGGL((naive ? (naive_kernel<TX, TY, BH, VEC>) : (wros_kernel<TX, TY, BH, VEC>)), grid,            \
-                           dim3(waves * 64), 0, st, p->d_indptr, p->d_cols, p->d_values_f32,                           \
-                           static_cast<const TX *>(X), ldx, static_cast<TY *>(Y), ldy, p->M, N, p->bw, rpr, ep);       \
+        hipLaunchKernelGGL((pick_kernel<TX, TY, BH, VEC>(naive)), grid, dim3(waves * 64), 0, st, p->d_indptr, p->d_cols,  \
+                           p->d_values_f32, static_cast<const TX *>(X), ldx, static_cast<TY *>(Y), ldy, p->M, N,       \
+                           p->bw, rpr, ep);                                                                            \
         break;
     switch (p->bh) {
         UBP_WROS_CASE(1) UBP_WROS_CASE(2) UBP_WROS_CASE(3) UBP_WROS_CASE(4) UBP_WROS_CASE(5) UBP_WROS_CASE(6)
@@ -176,11 +189,12 @@ ubp_status launch_wros_t(const ubp_packed *p, const void *X, int64_t ldx, int N,
 
 } // namespace
 
-ubp_status launch_wros(const ubp_packed *p, const void *X, int64_t ldx, int N, void *Y, int64_t ldy, ubp_dtype y_dtype,
+ubp_status UBP_LAUNCHER(launch_wros)(const ubp_packed *p, const void *X, int64_t ldx, int N, void *Y, int64_t ldy, ubp_dtype y_dtype,
                        int rpr, bool naive, const Epilogue &ep, void *stream, bool dry) {
     if (dry) return p->bh > 16 ? UBP_ERR_UNSUPPORTED : UBP_OK; // static LDS only: nothing to prepare
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (p->bh > 16) return UBP_ERR_UNSUPPORTED;
+    if (kWide && naive) return UBP_ERR_UNSUPPORTED;
     switch (p->dtype) {
     case UBP_F32: return launch_wros_t<float, float>(p, X, ldx, N, Y, ldy, rpr, naive, ep, st);
     case UBP_F16:
@@ -193,6 +207,7 @@ ubp_status launch_wros(const ubp_packed *p, const void *X, int64_t ldx, int N, v
     return UBP_ERR_INVALID_ARG;
 }
 
+#ifndef UBP_WIDE
 // An empty kernel: what a launch costs on this device with nothing to do (measurement only).
 __global__ void floor_kernel() {}
 
@@ -200,5 +215,6 @@ ubp_status launch_floor(void *stream) {
     hipLaunchKernelGGL(floor_kernel, dim3(1), dim3(64), 0, static_cast<hipStream_t>(stream));
     return hipGetLastError() == hipSuccess ? UBP_OK : UBP_ERR_DEVICE;
 }
+#endif
 
 } // namespace ubp

@@ -107,6 +107,8 @@ __global__ __launch_bounds__(1024) void wros4_kernel(Wros4Args a) {
     char *yrow = reinterpret_cast<char *>(a.Y) + (int64_t)i * a.ldy * 4;
     // (a lane without a pixel stores beyond the row's N pixels, which is dropped)
     const uint32_t ycol = PX == 64 || lane < PX ? (uint32_t)(col0 + lane % PX) * 4u : 0xfffffffcu;
+    [[maybe_unused]] Residual<float, 1> res;                 // of the next row of this wavefront's range, a row ahead
+    if constexpr (kWide) res.load(a.ep, lo, col0 + lane % PX, hi, a.N);
     auto finish = [&](int n) {                               // n rows are complete
         for (; n > 0; --n) {
             if ((uint32_t)(i - lo) < (uint32_t)(hi - lo)) {
@@ -114,7 +116,15 @@ __global__ __launch_bounds__(1024) void wros4_kernel(Wros4Args a) {
                 if (a.ep.on) {
                     int row = i;
                     asm volatile("" : "+s"(row)); // (no pointer into the bias is carried along where there is none)
-                    v = epilogue_value(a.ep, v, a.ep.bias ? a.ep.bias[row] : 0.f);
+                    const float b = a.ep.bias ? a.ep.bias[row] : 0.f;
+                    if constexpr (kWide) {
+                        float o[1] = {v};
+                        res.apply(a.ep, o, b);
+                        v = o[0];
+                        res.load(a.ep, row + 1, col0 + lane % PX, hi, a.N);
+                    } else {
+                        v = epilogue_value(a.ep, v, b);
+                    }
                 }
                 const __amdgpu_buffer_rsrc_t ry = __builtin_amdgcn_make_buffer_rsrc(yrow, 0, a.N * 4, 0x00020000);
                 __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), ry, ycol, 0, 0);
@@ -184,7 +194,7 @@ template <int BH> ubp_status launch_bh(const Wros4Args &a, int PX, int waves, hi
 
 } // namespace
 
-ubp_status launch_wros4(const Wros4Args &a, int bh, int PX, int waves, void *stream, bool dry) {
+ubp_status UBP_LAUNCHER(launch_wros4)(const Wros4Args &a, int bh, int PX, int waves, void *stream, bool dry) {
     hipStream_t st = static_cast<hipStream_t>(stream);
 #define UBP_WROS4_CASE(BH) \
     case BH: return launch_bh<BH>(a, PX, waves, st, dry);
