@@ -263,6 +263,71 @@ typedef struct {
 ubp_status ubp_linear(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t N, void *Y_dev, int64_t ldy,
                       ubp_dtype y_dtype, const ubp_linear_epilogue *epilogue, void *hip_stream, const ubp_plan *plan);
 
+/* ---------------------------------------------------------------------------------------------
+ * Training a pruned layer: the backward pass of Y = act(W X + bias) + residual at the weights that are kept.
+ *     Z = W X + bias    : ubp_spmm_fused with activation 0 (again in the backward pass, from a checkpoint of X)
+ *     G = dY act'(Z), dbias = sums of G's rows    : ubp_linear_grad
+ *     dW = G X^T at the kept weights              : ubp_weight_grad, ubp_weight_grad_checkpoint
+ *     dX = W^T G                                  : ubp_spmm with a handle of the transposed layer (ubp_pack of W^T with
+ *                                                   blocks (c, r) of bw x bh)
+ *     dresidual = dY
+ * As for ubp_spmm: device pointers, pitches in elements, any alignment of rows, work on hip_stream alone and no
+ * synchronisation; nothing is written on an error that a call returns before its launch.  A workspace is the caller's, 16-byte
+ * aligned, of at least the bytes that the function beside the call returns for this N (0: NULL will do); what it
+ * holds matters only while the call runs, and calls that may run at the same time need one each.  Results have the
+ * same bits from call to call.
+ */
+
+/*
+ * G = dY act'(Z) in the handle's type and dbias[i] = sum_n of the fp32 values of G[i][n] before they are rounded.
+ *   dY_dev, Z_dev, G_dev : M x N of the handle's type.  G may be dY or Z itself (the same pointer and pitch); no other overlap.
+ *   activation           : UBP_ACT_*, lo and hi as in ubp_linear.  ReLU's slope is 1 above 0, clamp's from lo to hi, both
+ *                          ends included; a slope of 0 gives G = 0 whatever dY is, and Z = NaN has slope 0.  UBP_ACT_NONE
+ *                          copies dY and does not read Z (NULL will do).  With the others NaN stays NaN.
+ *   dbias_dev            : M floats, overwritten, or NULL.
+ * N == 0: dbias becomes 0.  UBP_ERR_INVALID_ARG: null pointer, N < 0, pitch < N, lo > hi, workspace, host-only handle.
+ */
+int64_t ubp_linear_grad_workspace(const ubp_packed *p, int32_t N);
+ubp_status ubp_linear_grad(const ubp_packed *p, const void *dY_dev, int64_t lddy, const void *Z_dev, int64_t ldz, int32_t N,
+                           void *G_dev, int64_t ldg, float *dbias_dev, int32_t activation, float lo, float hi,
+                           void *workspace_dev, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * X (K x N of the handle's type) in 8 bits, for the backward pass: half the memory of 16 bits.
+ *   Q_dev : K x N bytes, pitch ldq (bytes, >= N): e4m3 codes (4 exponent bits, bias 7, 3 fraction bits, largest 448, 0x7f and
+ *           0xff NaN, no infinity).
+ *   S_dev : K x ceil(N / 32) bytes, pitch lds: s + 127 for each group of 32 neighbouring tokens of a row, s the smallest
+ *           exponent >= -127 with |x| <= 448 2^s for all finite x of the group.
+ * A code is x / 2^s to the nearest, ties to the even code; Inf and NaN become NaN and do not count for s.  Where 256 2^s
+ * is beyond the type (s = 8 for fp16, 120 for the others) codes stop at 240.  So |value - x| <= max(2^-4 |x|, 2^(s - 10)).
+ * load: X = value 2^s in the handle's type (rounded to nearest where fp16 has no such value).  save and load change nothing
+ * behind column N.  N == 0 is a no-op.  X, Q and S must not overlap.
+ */
+ubp_status ubp_checkpoint_save(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t N, uint8_t *Q_dev, int64_t ldq,
+                               uint8_t *S_dev, int64_t lds, void *hip_stream);
+ubp_status ubp_checkpoint_load(const ubp_packed *p, const uint8_t *Q_dev, int64_t ldq, const uint8_t *S_dev, int64_t lds, int32_t N,
+                               void *X_dev, int64_t ldx, void *hip_stream);
+
+/*
+ * dvalues[v] (+)= sum_n G[row of v][n] X[column of v][n], v over the canonical values (ubp_packed_values: the gradient of
+ * values[v] stands at v), in fp32.  G: M x N, X: K x N of the handle's type; or X as ubp_checkpoint_save left it, with the
+ * values that ubp_checkpoint_load gives.
+ *   dvalues_dev : nb * bh * bw floats, overwritten, or added to where accumulate != 0 (micro-batches).  Not part of G, X or
+ *                 the workspace.
+ * An Inf or NaN in G or X reaches only values in its own row or column of W.
+ * N == 0 sums nothing: zeros, or with accumulate nothing changes.  nb == 0 is a no-op.
+ * ubp_weight_grad_prepare (or the first call) builds and uploads the layout that the kernel reads, 1 KB per 16 x 16 tile that
+ * keeps weights; ubp_weight_grad_workspace builds it on the host.  UBP_ERR_UNSUPPORTED for 2^31 - 1 values or more (the workspace is
+ * then -1).
+ */
+int64_t ubp_weight_grad_workspace(const ubp_packed *p, int32_t N);
+ubp_status ubp_weight_grad_prepare(const ubp_packed *p);
+ubp_status ubp_weight_grad(const ubp_packed *p, const void *G_dev, int64_t ldg, const void *X_dev, int64_t ldx, int32_t N,
+                           float *dvalues_dev, int32_t accumulate, void *workspace_dev, int64_t workspace_bytes, void *hip_stream);
+ubp_status ubp_weight_grad_checkpoint(const ubp_packed *p, const void *G_dev, int64_t ldg, const uint8_t *Q_dev, int64_t ldq,
+                                      const uint8_t *S_dev, int64_t lds, int32_t N, float *dvalues_dev, int32_t accumulate,
+                                      void *workspace_dev, int64_t workspace_bytes, void *hip_stream);
+
 /*
  * Everything ubp_spmm_plan does with these arguments except the launch: resolves the kernel
  * and its shape, builds and uploads the re-layout of W that shape reads (host and device

@@ -26,7 +26,9 @@ EXPORTS = ("ubp_target_block_count", "ubp_select_reference", "ubp_pack", "ubp_pa
            "ubp_packed_free", "ubp_status_string", "ubp_packed_device_error", "ubp_packed_layout",
            "ubp_spmm_prepare", "ubp_launch_floor", "ubp_block_scores", "ubp_select_greedy", "ubp_select_bed",
            "ubp_select_optimal", "ubp_selection_to_blocks", "ubp_select_blocks", "ubp_selection_efficacy",
-           "ubp_spmm_fused", "ubp_linear")
+           "ubp_spmm_fused", "ubp_linear", "ubp_linear_grad_workspace", "ubp_linear_grad", "ubp_checkpoint_save",
+           "ubp_checkpoint_load", "ubp_weight_grad_workspace", "ubp_weight_grad_prepare", "ubp_weight_grad",
+           "ubp_weight_grad_checkpoint")
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "clamp": 2, "gelu": 3, "gelu_tanh": 4, "silu": 5}
 SELECT_METHODS = {"greedy": 0, "bed": 1, "optimal": 2}
 
@@ -98,6 +100,18 @@ def load_library():
     L.ubp_spmm_fused.restype = ctypes.c_int
     L.ubp_linear.argtypes = [vp, vp, i64, i32, vp, i64, ctypes.c_int, ctypes.POINTER(LinearEpilogue), vp, ctypes.POINTER(Plan)]
     L.ubp_linear.restype = ctypes.c_int
+    L.ubp_linear_grad.argtypes = [vp, vp, i64, vp, i64, i32, vp, i64, vp, i32, ctypes.c_float, ctypes.c_float, vp, i64, vp]
+    L.ubp_checkpoint_save.argtypes = [vp, vp, i64, i32, vp, i64, vp, i64, vp]
+    L.ubp_checkpoint_load.argtypes = [vp, vp, i64, vp, i64, i32, vp, i64, vp]
+    L.ubp_weight_grad_prepare.argtypes = [vp]
+    L.ubp_weight_grad.argtypes = [vp, vp, i64, vp, i64, i32, vp, i32, vp, i64, vp]
+    L.ubp_weight_grad_checkpoint.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, vp, i32, vp, i64, vp]
+    for f in (L.ubp_linear_grad, L.ubp_checkpoint_save, L.ubp_checkpoint_load, L.ubp_weight_grad_prepare, L.ubp_weight_grad,
+              L.ubp_weight_grad_checkpoint):
+        f.restype = ctypes.c_int
+    for f in (L.ubp_linear_grad_workspace, L.ubp_weight_grad_workspace):
+        f.argtypes = [vp, i32]
+        f.restype = i64
     L.ubp_launch_floor.argtypes = [vp]
     L.ubp_launch_floor.restype = ctypes.c_int
     L.ubp_block_scores.argtypes = [vp, ctypes.c_int, i64, i32, i32, i32, i32, i32, vp, i64]
@@ -360,6 +374,64 @@ def linear(packed, X_ptr, ldx, N, Y_ptr, ldy, y_dtype, bias_ptr=None, activation
                                    ctypes.byref(plan) if plan is not None else None)
     if rc != UBP_OK:
         raise UBPError(rc, "ubp_linear")
+
+
+def _workspace(name, packed, N):
+    n = int(getattr(load_library(), name)(packed.handle, N))
+    if n < 0:
+        raise UBPError(1, name)
+    return n
+
+
+def _call(name, *args):
+    rc = getattr(load_library(), name)(*args)
+    if rc != UBP_OK:
+        raise UBPError(rc, name)
+
+
+def linear_grad_workspace(packed, N):
+    """ubp_linear_grad_workspace -> bytes (0: none needed)."""
+    return _workspace("ubp_linear_grad_workspace", packed, N)
+
+
+def linear_grad(packed, dY_ptr, lddy, Z_ptr, ldz, N, G_ptr, ldg, dbias_ptr=None, activation=None, lo=0.0, hi=0.0,
+                workspace_ptr=None, workspace_bytes=0, stream=0):
+    """ubp_linear_grad with raw DEVICE pointers: G = dY act'(Z), dbias = sums of G's rows (or None)."""
+    _call("ubp_linear_grad", packed.handle, dY_ptr, lddy, Z_ptr, ldz, N, G_ptr, ldg, dbias_ptr, ACTIVATIONS[activation], float(lo),
+          float(hi), workspace_ptr, workspace_bytes, stream)
+
+
+def checkpoint_save(packed, X_ptr, ldx, N, Q_ptr, ldq, S_ptr, lds, stream=0):
+    """ubp_checkpoint_save with raw DEVICE pointers: X (K x N) to e4m3 codes and an exponent byte per 32 tokens."""
+    _call("ubp_checkpoint_save", packed.handle, X_ptr, ldx, N, Q_ptr, ldq, S_ptr, lds, stream)
+
+
+def checkpoint_load(packed, Q_ptr, ldq, S_ptr, lds, N, X_ptr, ldx, stream=0):
+    """ubp_checkpoint_load with raw DEVICE pointers: the values of a checkpoint in the handle's type."""
+    _call("ubp_checkpoint_load", packed.handle, Q_ptr, ldq, S_ptr, lds, N, X_ptr, ldx, stream)
+
+
+def weight_grad_workspace(packed, N):
+    """ubp_weight_grad_workspace -> bytes (0: none needed)."""
+    return _workspace("ubp_weight_grad_workspace", packed, N)
+
+
+def weight_grad_prepare(packed):
+    """ubp_weight_grad_prepare: everything the first ubp_weight_grad does beside its launch."""
+    _call("ubp_weight_grad_prepare", packed.handle)
+
+
+def weight_grad(packed, G_ptr, ldg, X_ptr, ldx, N, dvalues_ptr, accumulate=False, workspace_ptr=None, workspace_bytes=0, stream=0):
+    """ubp_weight_grad with raw DEVICE pointers: the gradient of Packed.values, in fp32."""
+    _call("ubp_weight_grad", packed.handle, G_ptr, ldg, X_ptr, ldx, N, dvalues_ptr, int(bool(accumulate)), workspace_ptr,
+          workspace_bytes, stream)
+
+
+def weight_grad_checkpoint(packed, G_ptr, ldg, Q_ptr, ldq, S_ptr, lds, N, dvalues_ptr, accumulate=False, workspace_ptr=None,
+                           workspace_bytes=0, stream=0):
+    """ubp_weight_grad_checkpoint: the same with X as checkpoint_save left it."""
+    _call("ubp_weight_grad_checkpoint", packed.handle, G_ptr, ldg, Q_ptr, ldq, S_ptr, lds, N, dvalues_ptr, int(bool(accumulate)),
+          workspace_ptr, workspace_bytes, stream)
 
 
 def spmm_prepare(packed, X_ptr, ldx, N, Y_ptr, ldy, y_dtype, plan=None):

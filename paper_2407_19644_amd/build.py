@@ -10,8 +10,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libubp.so")
-HOST_SOURCES = ["ubp_host.cpp", "ubp_layouts.cpp", "ubp_choose.cpp", "ubp_select.cpp"]
-HIP_SOURCES = ["ubp_api.hip", "ubp_wros.hip", "ubp_wros4.hip", "ubp_stripe.hip", "ubp_blk.hip", "ubp_tile.hip", "ubp_direct.hip", "ubp_mtile.hip"]
+HOST_SOURCES = ["ubp_host.cpp", "ubp_layouts.cpp", "ubp_grad_layout.cpp", "ubp_choose.cpp", "ubp_select.cpp"]
+HIP_SOURCES = ["ubp_api.hip", "ubp_wros.hip", "ubp_wros4.hip", "ubp_stripe.hip", "ubp_blk.hip", "ubp_tile.hip", "ubp_direct.hip", "ubp_mtile.hip",
+               "ubp_wgrad.hip", "ubp_train.hip"]
 # compiled a second time with UBP_WIDE: the epilogue with activations beyond a clamp and a residual
 WIDE_SOURCES = ["ubp_wros.hip", "ubp_wros4.hip", "ubp_stripe.hip", "ubp_blk.hip", "ubp_tile.hip", "ubp_direct.hip", "ubp_mtile.hip"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result"]

@@ -197,6 +197,28 @@ ubp_status upload_wros4_layout(const ubp_packed *p) {
     return UBP_OK;
 }
 
+ubp_status upload_grad_layout(const ubp_packed *p) {
+    GradLayoutDev &D = p->d_grad;
+    if (D.uploaded) return UBP_OK;
+    const GradLayout &L = p->grad;
+    const bool ok = (D.regions || dev_copy_vec(&D.regions, L.regions, &p->device_bytes)) && (D.rows || dev_copy_vec(&D.rows, L.rows, &p->device_bytes)) &&
+                    (D.ops || dev_copy_vec(&D.ops, L.ops, &p->device_bytes)) && (D.inv || dev_copy_vec(&D.inv, L.inv, &p->device_bytes));
+    if (!ok) {
+        (void)hipGetLastError();
+        auto drop = [](auto *&ptr) {
+            if (ptr) (void)hipFree(ptr);
+            ptr = nullptr;
+        };
+        drop(D.regions);
+        drop(D.rows);
+        drop(D.ops);
+        drop(D.inv);
+        return UBP_ERR_ALLOC;
+    }
+    D.uploaded = true;
+    return UBP_OK;
+}
+
 void release_device(ubp_packed *p) {
     if (!p || p->device == UBP_HOST_ONLY) return;
     DeviceGuard guard(p->device);
@@ -216,6 +238,10 @@ void release_device(ubp_packed *p) {
     rel(p->d_direct.ids);
     rel(p->d_direct.frags);
     rel(p->d_wros4.weights);
+    rel(p->d_grad.regions);
+    rel(p->d_grad.rows);
+    rel(p->d_grad.ops);
+    rel(p->d_grad.inv);
     for (int s = 0; s < kNumLayouts; ++s) {
         rel(p->d_sg[s].rg_ptr);
         rel(p->d_sg[s].rg_order);
@@ -500,6 +526,137 @@ ubp_status execute(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t 
     return UBP_ERR_ALLOC;
 }
 
+// ------------------------------------------------------------------ training
+// Workgroups of a row of the epilogue's gradient: one per row where the rows fill the card by themselves, else one per 4 chunks
+// (256 rows of 12544 tokens: see the kernel).
+int act_row_groups(int M, int N) {
+    const int chunks = (int)(((int64_t)N + kActChunk - 1) / kActChunk);
+    return M >= 1024 || chunks <= 4 ? 1 : (chunks + 3) / 4;
+}
+
+ubp_status linear_grad(const ubp_packed *p, const void *dY, int64_t lddy, const void *Z, int64_t ldz, int32_t N, void *G, int64_t ldg,
+                       float *dbias, int32_t activation, float lo, float hi, void *workspace, int64_t workspace_bytes, void *stream) {
+    if (!p || p->device == UBP_HOST_ONLY || N < 0) return UBP_ERR_INVALID_ARG;
+    if (activation < UBP_ACT_NONE || activation > UBP_ACT_SILU) return UBP_ERR_INVALID_ARG;
+    if (activation == UBP_ACT_CLAMP && !(lo <= hi)) return UBP_ERR_INVALID_ARG;
+    if (N > 0) {
+        if (!dY || !G || lddy < N || ldg < N) return UBP_ERR_INVALID_ARG;
+        if (activation != UBP_ACT_NONE && (!Z || ldz < N)) return UBP_ERR_INVALID_ARG;
+    }
+    if (N == 0 && !dbias) return UBP_OK;
+    ActGradArgs a = {};
+    a.dY = dY;
+    a.Z = Z;
+    a.G = G;
+    a.lddy = lddy;
+    a.ldz = ldz;
+    a.ldg = ldg;
+    a.M = p->M;
+    a.N = N;
+    activation_of(activation, a.act, a.c1, a.c3);
+    a.pass = activation == UBP_ACT_NONE ? kPassAll : activation == UBP_ACT_RELU ? kPassAbove : kPassInside;
+    a.lo = activation == UBP_ACT_CLAMP ? lo : 0.f;
+    a.hi = activation == UBP_ACT_CLAMP ? hi : INFINITY;
+    a.dbias = dbias;
+    a.row_groups = act_row_groups(p->M, N);
+    a.group_chunks = a.row_groups > 1 ? 4 : std::max(1, (int)(((int64_t)N + kActChunk - 1) / kActChunk));
+    if (dbias && a.row_groups > 1) {
+        if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0 || workspace_bytes < (int64_t)p->M * a.row_groups * 4)
+            return UBP_ERR_INVALID_ARG;
+        a.part = static_cast<float *>(workspace);
+    }
+    DeviceGuard guard(p->device);
+    if (!guard.ok) return UBP_ERR_DEVICE;
+    return launch_act_grad(a, p->dtype, stream);
+}
+
+ubp_status checkpoint(const ubp_packed *p, bool save, void *X, int64_t ldx, int32_t N, uint8_t *Q, int64_t ldq, uint8_t *S, int64_t lds,
+                      void *stream) {
+    if (!p || p->device == UBP_HOST_ONLY || N < 0) return UBP_ERR_INVALID_ARG;
+    if (N == 0) return UBP_OK;
+    if (!X || !Q || !S || ldx < N || ldq < N || lds < ((int64_t)N + 31) / 32) return UBP_ERR_INVALID_ARG;
+    CheckpointArgs a = {};
+    a.X = save ? X : nullptr;
+    a.out = save ? nullptr : X;
+    a.Q = Q;
+    a.S = S;
+    a.ldx = ldx;
+    a.ldq = ldq;
+    a.lds = lds;
+    a.K = p->K;
+    a.N = N;
+    DeviceGuard guard(p->device);
+    if (!guard.ok) return UBP_ERR_DEVICE;
+    return save ? launch_save(a, p->dtype, stream) : launch_load(a, p->dtype, stream);
+}
+
+// Tokens of a step of the weight gradient: 64 bytes of a row.
+int64_t grad_steps(const ubp_packed *p, int32_t N) {
+    const int64_t per = 64 / dtype_size(p->dtype);
+    return ((int64_t)N + per - 1) / per;
+}
+
+ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const void *X, int64_t ldx, const uint8_t *S, int64_t lds, bool saved,
+                       int32_t N, float *dvalues, int32_t accumulate, void *workspace, int64_t workspace_bytes, void *stream, bool dry) try {
+    if (!p || p->device == UBP_HOST_ONLY || N < 0) return UBP_ERR_INVALID_ARG;
+    if (!dry && p->nb == 0) return UBP_OK;
+    if (!dry && !dvalues) return UBP_ERR_INVALID_ARG;
+    if (N > 0 && !dry) {
+        if (!G || !X || ldg < N || ldx < N) return UBP_ERR_INVALID_ARG;
+        if (saved && (!S || lds < ((int64_t)N + 31) / 32)) return UBP_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(p->device);
+    if (!guard.ok) return UBP_ERR_DEVICE;
+    const GradLayout *L = nullptr;
+    {
+        std::lock_guard<std::mutex> hold(p->lock);
+        L = &get_grad_layout(p);
+        if (!L->usable) return UBP_ERR_UNSUPPORTED;
+        const ubp_status rc = upload_grad_layout(p);
+        if (rc != UBP_OK) return rc;
+    }
+    GradArgs a = {};
+    a.regions = p->d_grad.regions;
+    a.rows = p->d_grad.rows;
+    a.inv = p->d_grad.inv;
+    a.ops = p->d_grad.ops;
+    a.G = G;
+    a.X = X;
+    a.S = S;
+    a.ldg = ldg;
+    a.ldx = ldx;
+    a.lds = lds;
+    a.N = N;
+    a.n_regions = L->n_regions;
+    a.slots = L->max_slots;
+    a.n_tiles = L->n_tiles;
+    a.out = dvalues;
+    a.accumulate = accumulate ? 1 : 0;
+    if (dry) {
+        ubp_status rc = launch_weight_grad(a, p->dtype, false, L->max_tiles, stream, true);
+        if (rc == UBP_OK) rc = launch_weight_grad(a, p->dtype, true, L->max_tiles, stream, true);
+        return rc;
+    }
+    if (N == 0) {
+        if (accumulate) return UBP_OK;
+        return launch_weight_sum(a, stream); // (a sum of no ranges)
+    }
+    const int64_t steps = grad_steps(p, N);
+    a.splits = grad_splits(*L, steps);
+    a.per_split = (int)((steps + a.splits - 1) / a.splits);
+    if (a.splits > 1) {
+        if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0 || workspace_bytes < a.splits * L->n_tiles * 1024) return UBP_ERR_INVALID_ARG;
+        a.part = static_cast<float *>(workspace);
+    }
+    const ubp_status rc = launch_weight_grad(a, p->dtype, saved, L->max_tiles, stream, false);
+    if (rc != UBP_OK || a.splits == 1) return rc;
+    return launch_weight_sum(a, stream);
+} catch (const std::bad_alloc &) {
+    return UBP_ERR_ALLOC;
+} catch (const std::length_error &) {
+    return UBP_ERR_ALLOC;
+}
+
 } // namespace
 
 } // namespace ubp
@@ -533,6 +690,59 @@ ubp_status ubp_spmm_fused(const ubp_packed *p, const void *X_dev, int64_t ldx, i
 ubp_status ubp_linear(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t N, void *Y_dev, int64_t ldy,
                       ubp_dtype y_dtype, const ubp_linear_epilogue *epilogue, void *hip_stream, const ubp_plan *plan) {
     return ubp::execute(p, X_dev, ldx, N, Y_dev, ldy, y_dtype, hip_stream, plan, false, nullptr, epilogue);
+}
+
+int64_t ubp_linear_grad_workspace(const ubp_packed *p, int32_t N) {
+    if (!p || N < 0) return -1;
+    const int groups = ubp::act_row_groups(p->M, N);
+    return groups > 1 ? (int64_t)p->M * groups * 4 : 0;
+}
+
+ubp_status ubp_linear_grad(const ubp_packed *p, const void *dY_dev, int64_t lddy, const void *Z_dev, int64_t ldz, int32_t N,
+                           void *G_dev, int64_t ldg, float *dbias_dev, int32_t activation, float lo, float hi,
+                           void *workspace_dev, int64_t workspace_bytes, void *hip_stream) {
+    return ubp::linear_grad(p, dY_dev, lddy, Z_dev, ldz, N, G_dev, ldg, dbias_dev, activation, lo, hi, workspace_dev, workspace_bytes,
+                            hip_stream);
+}
+
+ubp_status ubp_checkpoint_save(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t N, uint8_t *Q_dev, int64_t ldq,
+                               uint8_t *S_dev, int64_t lds, void *hip_stream) {
+    return ubp::checkpoint(p, true, const_cast<void *>(X_dev), ldx, N, Q_dev, ldq, S_dev, lds, hip_stream);
+}
+
+ubp_status ubp_checkpoint_load(const ubp_packed *p, const uint8_t *Q_dev, int64_t ldq, const uint8_t *S_dev, int64_t lds, int32_t N,
+                               void *X_dev, int64_t ldx, void *hip_stream) {
+    return ubp::checkpoint(p, false, X_dev, ldx, N, const_cast<uint8_t *>(Q_dev), ldq, const_cast<uint8_t *>(S_dev), lds, hip_stream);
+}
+
+int64_t ubp_weight_grad_workspace(const ubp_packed *p, int32_t N) {
+    if (!p || N < 0) return -1;
+    try {
+        std::lock_guard<std::mutex> hold(p->lock);
+        const ubp::GradLayout &L = ubp::get_grad_layout(p);
+        if (!L.usable) return -1;
+        const int splits = ubp::grad_splits(L, ubp::grad_steps(p, N));
+        return splits > 1 ? splits * L.n_tiles * 1024 : 0;
+    } catch (...) {
+        return -1;
+    }
+}
+
+ubp_status ubp_weight_grad_prepare(const ubp_packed *p) {
+    return ubp::weight_grad(p, nullptr, 0, nullptr, 0, nullptr, 0, false, 0, nullptr, 0, nullptr, 0, nullptr, true);
+}
+
+ubp_status ubp_weight_grad(const ubp_packed *p, const void *G_dev, int64_t ldg, const void *X_dev, int64_t ldx, int32_t N,
+                           float *dvalues_dev, int32_t accumulate, void *workspace_dev, int64_t workspace_bytes, void *hip_stream) {
+    return ubp::weight_grad(p, G_dev, ldg, X_dev, ldx, nullptr, 0, false, N, dvalues_dev, accumulate, workspace_dev, workspace_bytes,
+                            hip_stream, false);
+}
+
+ubp_status ubp_weight_grad_checkpoint(const ubp_packed *p, const void *G_dev, int64_t ldg, const uint8_t *Q_dev, int64_t ldq,
+                                      const uint8_t *S_dev, int64_t lds, int32_t N, float *dvalues_dev, int32_t accumulate,
+                                      void *workspace_dev, int64_t workspace_bytes, void *hip_stream) {
+    return ubp::weight_grad(p, G_dev, ldg, Q_dev, ldq, S_dev, lds, true, N, dvalues_dev, accumulate, workspace_dev, workspace_bytes,
+                            hip_stream, false);
 }
 
 ubp_status ubp_spmm_prepare(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t N, void *Y_dev, int64_t ldy,

@@ -1,0 +1,205 @@
+// Host side of the weight gradient: which products of rows of G and X it forms, cut into regions for the workgroups.
+#include <algorithm>
+#include <cstdint>
+#include <vector>
+
+#include "ubp_internal.h"
+
+namespace ubp {
+
+namespace {
+
+// A tile before regions are cut: rows r0 .. r0 + 15 of G with up to 16 rows of X (columns of W).
+struct Tile {
+    int32_t r0;
+    int32_t col[16];
+    int32_t n; // columns used
+};
+
+// Rows of X that a run of tiles needs, ascending; rows of G likewise (numbers of M and above, of windows that reach
+// over the bottom edge, included).
+void union_of(const std::vector<Tile> &tiles, const int32_t *order, int64_t n, std::vector<int32_t> &g, std::vector<int32_t> &x) {
+    g.clear();
+    x.clear();
+    for (int64_t t = 0; t < n; ++t) {
+        const Tile &a = tiles[(size_t)order[t]];
+        for (int i = 0; i < kStripe; ++i) g.push_back(a.r0 + i);
+        x.insert(x.end(), a.col, a.col + a.n);
+    }
+    for (auto *v : {&g, &x}) {
+        std::sort(v->begin(), v->end());
+        v->erase(std::unique(v->begin(), v->end()), v->end());
+    }
+}
+
+int64_t padded(size_t n) { return ((int64_t)n + 15) / 16 * 16; }
+
+struct Region {
+    int64_t first, n; // run of the tile order
+    int64_t slots;    // LDS rows
+};
+
+} // namespace
+
+// Windows of 16 rows start every 17 - bh rows, so that each block lies inside one of them; a block of more than 16 rows is
+// cut into runs of 16, each a window.  The columns in which a window keeps weights, 16 at a time, are its tiles.
+// Regions: the tiles are halved again and again, by rows or by columns, whichever needs fewer rows of G and X
+// afterwards, until there are enough and each fits a workgroup's registers and LDS.
+const GradLayout &get_grad_layout(const ubp_packed *p) {
+    GradLayout &L = p->grad;
+    if (L.built) return L;
+    GradLayout out;
+    out.built = true;
+    const int64_t values = p->nb * p->bh * p->bw;
+    if (values >= (int64_t(1) << 31) - 1) { // (places of values are 32-bit numbers)
+        L = std::move(out);
+        return L;
+    }
+    out.usable = true;
+    const int bh = p->bh, bw = p->bw;
+    const int stride = bh <= kStripe ? kStripe + 1 - bh : 1;
+    // pieces of blocks by window, in canonical order: rows first, then columns
+    struct Piece { int32_t r0, b; };
+    std::vector<Piece> pieces;
+    {
+        int32_t r = 0;
+        for (int64_t b = 0; b < p->nb; ++b) {
+            while (p->indptr[(size_t)r + 1] <= b) ++r;
+            if (bh <= kStripe) {
+                pieces.push_back({r / stride * stride, (int32_t)b});
+            } else {
+                for (int k = 0; k < bh; k += kStripe) pieces.push_back({r + k, (int32_t)b});
+            }
+        }
+    }
+    std::vector<int32_t> start((size_t)p->nb);
+    {
+        int32_t r = 0;
+        for (int64_t b = 0; b < p->nb; ++b) {
+            while (p->indptr[(size_t)r + 1] <= b) ++r;
+            start[(size_t)b] = r;
+        }
+    }
+    std::stable_sort(pieces.begin(), pieces.end(), [](const Piece &a, const Piece &b) { return a.r0 < b.r0; });
+    std::vector<Tile> tiles;
+    std::vector<int32_t> inv; // of the tiles in this order
+    std::vector<int32_t> slot_of((size_t)p->K, -1), cols;
+    for (size_t i = 0; i < pieces.size();) {
+        size_t j = i;
+        cols.clear();
+        for (; j < pieces.size() && pieces[j].r0 == pieces[i].r0; ++j)
+            for (int q = 0; q < bw; ++q) cols.push_back(p->indices[(size_t)pieces[j].b] + q);
+        std::sort(cols.begin(), cols.end());
+        cols.erase(std::unique(cols.begin(), cols.end()), cols.end());
+        const size_t tile0 = tiles.size();
+        for (size_t c = 0; c < cols.size(); ++c) {
+            if (c % 16 == 0) tiles.push_back({pieces[i].r0, {0}, 0});
+            Tile &t = tiles.back();
+            t.col[t.n++] = cols[c];
+            slot_of[(size_t)cols[c]] = (int32_t)c;
+        }
+        inv.resize(tiles.size() * 256, -1);
+        for (size_t k = i; k < j; ++k) {
+            const int64_t b = pieces[k].b;
+            const int32_t first = std::max(start[(size_t)b], pieces[k].r0), last = std::min(start[(size_t)b] + bh, pieces[k].r0 + kStripe);
+            for (int q = 0; q < bw; ++q) {
+                const int32_t c = slot_of[(size_t)(p->indices[(size_t)b] + q)];
+                int32_t *t = &inv[(tile0 + (size_t)(c / 16)) * 256];
+                for (int32_t row = first; row < last; ++row) {
+                    const int e = row - pieces[k].r0;
+                    t[(16 * (e >> 2) + c % 16) * 4 + (e & 3)] = (int32_t)((b * bw + q) * bh + row % bh);
+                }
+            }
+        }
+        i = j;
+    }
+    const int64_t n = (int64_t)tiles.size();
+    out.n_tiles = n;
+    std::vector<int32_t> order((size_t)n);
+    for (int64_t t = 0; t < n; ++t) order[(size_t)t] = (int32_t)t;
+    std::vector<Region> done, open;
+    std::vector<int32_t> g, x, by_row, by_col;
+    auto slots = [&](const int32_t *o, int64_t count) {
+        union_of(tiles, o, count, g, x);
+        return padded(g.size()) + padded(x.size());
+    };
+    if (n) open.push_back({0, n, slots(order.data(), n)});
+    // the workgroups of a split of the tokens are as many as an XCD has CUs, while a wavefront keeps two tiles at least
+    const int64_t wanted = std::min<int64_t>(kGradRegions, (n + 2 * kGradWaves - 1) / (2 * kGradWaves));
+    while (!open.empty()) {
+        // the largest one next
+        size_t at = 0;
+        for (size_t k = 1; k < open.size(); ++k)
+            if (open[k].n > open[at].n) at = k;
+        const Region r = open[at];
+        const bool fits = r.n <= (int64_t)kGradWaves * kGradMaxTiles && r.slots <= kGradMaxSlots;
+        if ((fits && (int64_t)(open.size() + done.size()) >= wanted) || r.n == 1) {
+            done.push_back(r);
+            open.erase(open.begin() + (ptrdiff_t)at);
+            continue;
+        }
+        // halves by rows, and by columns
+        int32_t *o = &order[(size_t)r.first];
+        by_row.assign(o, o + r.n);
+        by_col = by_row;
+        std::sort(by_row.begin(), by_row.end(), [&](int32_t a, int32_t b) {
+            const Tile &s = tiles[(size_t)a], &t = tiles[(size_t)b];
+            return s.r0 != t.r0 ? s.r0 < t.r0 : s.col[0] < t.col[0];
+        });
+        std::sort(by_col.begin(), by_col.end(), [&](int32_t a, int32_t b) {
+            const Tile &s = tiles[(size_t)a], &t = tiles[(size_t)b];
+            return s.col[0] != t.col[0] ? s.col[0] < t.col[0] : s.r0 < t.r0;
+        });
+        const int64_t half = (r.n + 1) / 2;
+        const int64_t rows[2] = {slots(by_row.data(), half), slots(by_row.data() + half, r.n - half)};
+        const int64_t cs[2] = {slots(by_col.data(), half), slots(by_col.data() + half, r.n - half)};
+        const bool rows_win = rows[0] + rows[1] <= cs[0] + cs[1];
+        std::copy(rows_win ? by_row.begin() : by_col.begin(), rows_win ? by_row.end() : by_col.end(), o);
+        open[at] = {r.first, half, rows_win ? rows[0] : cs[0]};
+        open.push_back({r.first + half, r.n - half, rows_win ? rows[1] : cs[1]});
+    }
+    std::sort(done.begin(), done.end(), [](const Region &a, const Region &b) { return a.first < b.first; });
+    out.inv.resize((size_t)n * 256);
+    out.ops.resize((size_t)n * 16);
+    std::vector<int32_t> slot_x((size_t)p->K, 0);
+    for (const Region &r : done) {
+        int32_t *o = &order[(size_t)r.first];
+        // tiles of one window side by side
+        std::sort(o, o + r.n, [&](int32_t a, int32_t b) {
+            const Tile &s = tiles[(size_t)a], &t = tiles[(size_t)b];
+            return s.r0 != t.r0 ? s.r0 < t.r0 : s.col[0] < t.col[0];
+        });
+        union_of(tiles, o, r.n, g, x);
+        const int32_t first_slot = (int32_t)out.rows.size();
+        const int32_t g_slots = (int32_t)padded(g.size()), all = g_slots + (int32_t)padded(x.size());
+        for (int32_t v : g) out.rows.push_back(v < p->M ? v : -1);
+        out.rows.resize((size_t)first_slot + (size_t)g_slots, -1);
+        for (size_t k = 0; k < x.size(); ++k) slot_x[(size_t)x[k]] = g_slots + (int32_t)k;
+        out.rows.insert(out.rows.end(), x.begin(), x.end());
+        out.rows.resize((size_t)first_slot + (size_t)all, -1);
+        for (int64_t t = 0; t < r.n; ++t) {
+            const Tile &a = tiles[(size_t)o[t]];
+            const int64_t to = r.first + t;
+            const int32_t g0 = (int32_t)(std::lower_bound(g.begin(), g.end(), a.r0) - g.begin());
+            for (int k = 0; k < 16; ++k)
+                out.ops[(size_t)(to * 16 + k)] = (uint32_t)(g0 + k) | (uint32_t)slot_x[(size_t)a.col[k < a.n ? k : 0]] << 16;
+            std::copy(&inv[(size_t)o[t] * 256], &inv[(size_t)o[t] * 256] + 256, &out.inv[(size_t)to * 256]);
+        }
+        out.regions.insert(out.regions.end(), {(int32_t)r.first, (int32_t)r.n, first_slot, g_slots, all, 0, 0, 0});
+        out.max_tiles = std::max(out.max_tiles, (int)((r.n + kGradWaves - 1) / kGradWaves));
+        out.max_slots = std::max(out.max_slots, (int)all);
+    }
+    out.n_regions = (int)done.size();
+    L = std::move(out);
+    return L;
+}
+
+// Ranges of tokens that the sum is cut into: the regions of all ranges fill the CUs about once, and a range has at least
+// kGradMinSteps steps.
+int grad_splits(const GradLayout &L, int64_t steps) {
+    if (L.n_regions == 0 || steps <= 0) return 1;
+    const int64_t fill = std::max<int64_t>(1, kGradWorkgroups / L.n_regions);
+    return (int)std::max<int64_t>(1, std::min(fill, steps / kGradMinSteps));
+}
+
+} // namespace ubp

@@ -215,6 +215,33 @@ struct Wros4Layout {
     std::vector<int32_t> rec_of_row, rec_of_end, row_of_rec;
 };
 
+// Weight gradient: wavefronts of a workgroup, tiles a wavefront keeps at most, LDS rows (of 64 bytes, two buffers) of a
+// region at most, regions that a layer is cut into where its tiles allow, workgroups that fill the card, steps of a range of
+// tokens at least.
+constexpr int kGradWaves = 8;
+constexpr int kGradMaxTiles = 28;
+constexpr int kGradMaxSlots = 1264;
+constexpr int kGradRegions = 32;
+constexpr int kGradWorkgroups = 256;
+constexpr int kGradMinSteps = 4;
+
+// Host image of the weight gradient's layout.  A tile is the product of 16 consecutive rows of G with 16 rows of X; a region
+// is a run of tiles that one workgroup keeps in registers, with the rows of G and X that they need.
+//   regions : 8 words each: first tile, tiles, first entry of rows, entries for G (a multiple of 16), for G and X (likewise)
+//   rows    : row of G, then of X, per LDS row of the region; -1 for one that holds zeros
+//   ops     : 16 words per tile: LDS row of G | LDS row of X << 16
+//   inv     : 256 words per tile: the value that element (16 (i / 4) + j) 4 + i % 4, row i and column j of the tile,
+//             is the gradient of (a place in the canonical values), -1 for none.  Every value appears once.
+struct GradLayout {
+    bool built = false, usable = false;
+    int64_t n_tiles = 0;
+    int n_regions = 0;
+    int max_tiles = 0; // of a wavefront
+    int max_slots = 0; // LDS rows of a region
+    std::vector<int32_t> regions, rows, inv;
+    std::vector<uint32_t> ops;
+};
+
 struct StripeLayoutDev {
     int32_t *rg_ptr = nullptr;
     int32_t *rg_order = nullptr;
@@ -239,6 +266,11 @@ struct Wros4LayoutDev {
     float *weights = nullptr; // (the allocation; the others lie behind them)
     const uint32_t *offsets = nullptr;
     const int32_t *rec_of_row = nullptr, *rec_of_end = nullptr, *row_of_rec = nullptr;
+};
+struct GradLayoutDev {
+    int32_t *regions = nullptr, *rows = nullptr, *inv = nullptr;
+    uint32_t *ops = nullptr;
+    bool uploaded = false;
 };
 struct TileLayoutDev {
     uint16_t *frags = nullptr;
@@ -353,6 +385,45 @@ struct TileArgs {
     Epilogue ep;
 };
 
+// The weight gradient's kernel and the sum over its ranges of tokens.
+struct GradArgs {
+    const int32_t *regions, *rows, *inv;
+    const uint32_t *ops;
+    const void *G, *X;        // X: rows of the layer's type, or of a checkpoint's bytes
+    const uint8_t *S;         // the checkpoint's exponents
+    int64_t ldg, ldx, lds;
+    int N, n_regions, splits;
+    int per_split;            // steps of a range
+    int slots;                // LDS rows of a buffer
+    int64_t n_tiles;
+    float *out;               // dvalues
+    float *part;              // [splits][tiles][256], where splits > 1
+    int accumulate;
+};
+
+// Gradient of the epilogue.  pass, for kActClamp: what the slope is 1 for.
+enum : int { kPassInside = 0, kPassAbove = 1, kPassAll = 2 }; // lo <= z <= hi; z > lo; everything (Z is not read)
+struct ActGradArgs {
+    const void *dY, *Z;
+    void *G;
+    int64_t lddy, ldz, ldg;
+    int M, N, act, pass;
+    float c1, c3, lo, hi;
+    float *dbias, *part;      // part: [M][row_groups], where row_groups > 1
+    int row_groups, group_chunks; // workgroups of a long row, chunks of kActChunk tokens of each
+};
+constexpr int kActChunk = 2048;
+
+// A checkpoint: X -> Q, S, or Q, S -> out (pitch ldx).
+struct CheckpointArgs {
+    const void *X;
+    uint8_t *Q, *S;
+    void *out;
+    int64_t ldx, ldq, lds;
+    int K, N;
+    int units;                // wavefronts of a row
+};
+
 // What a call resolves to: the kernel and its launch shape, every field set.
 struct Shape {
     int kernel = 0;   // 1 vector, 2 gather, 4 small-K dense tiles, 5 / 7 / 9 dense tiles through LDS, 6 block, 8 direct
@@ -393,6 +464,7 @@ struct ubp_packed {
     mutable ubp::TileLayout tiles;
     mutable ubp::DirectLayout direct;
     mutable ubp::Wros4Layout wros4;
+    mutable ubp::GradLayout grad;
     mutable ubp::MaskStats stats;
     mutable ubp::Choice choices[ubp::kChoices];
     mutable int next_choice = 0;
@@ -406,6 +478,7 @@ struct ubp_packed {
     mutable ubp::TileLayoutDev d_tiles;
     mutable ubp::DirectLayoutDev d_direct;
     mutable ubp::Wros4LayoutDev d_wros4;
+    mutable ubp::GradLayoutDev d_grad;
     uint32_t *d_error = nullptr;   // set by a kernel whose bounded wait ran out
     mutable int64_t device_bytes = 0;
 };
@@ -423,6 +496,8 @@ const BlkLayout &get_blk_layout(const ubp_packed *p, int G);
 const TileLayout &get_tile_layout(const ubp_packed *p);
 const DirectLayout &get_direct_layout(const ubp_packed *p);
 const Wros4Layout &get_wros4_layout(const ubp_packed *p);
+const GradLayout &get_grad_layout(const ubp_packed *p);
+int grad_splits(const GradLayout &L, int64_t steps);
 const MaskStats &get_mask_stats(const ubp_packed *p);
 // Stripes per wavefront of the gather kernel.  They follow the block height: a 16-row block touches two stripes
 // anyway, so tall row groups cost little extra zero fill and divide the staging of X by the rows a workgroup
@@ -444,6 +519,7 @@ ubp_status upload_blk_layout(const ubp_packed *p, int slot);
 ubp_status upload_tile_layout(const ubp_packed *p);
 ubp_status upload_direct_layout(const ubp_packed *p);
 ubp_status upload_wros4_layout(const ubp_packed *p);
+ubp_status upload_grad_layout(const ubp_packed *p);
 
 // Launchers.  `dry` only raises the kernels' dynamic LDS limit on the current device (what a
 // first launch of a shape would do), so that a later launch is nothing but a launch.
@@ -459,6 +535,11 @@ struct MtileShape { int rows, pixels, per_cu; };
 constexpr int kNumMtileShapes = 5;
 constexpr MtileShape kMtileShapes[kNumMtileShapes] = {{128, 128, 1}, {128, 64, 1}, {64, 128, 1}, {64, 64, 2}, {128, 256, 1}};
 ubp_status launch_mtile(const TileArgs &a, bool bf16, bool y_f32, int shape, int rows, void *stream, bool dry);
+ubp_status launch_weight_grad(const GradArgs &a, ubp_dtype dtype, bool checkpoint, int max_tiles, void *stream, bool dry);
+ubp_status launch_weight_sum(const GradArgs &a, void *stream);
+ubp_status launch_act_grad(const ActGradArgs &a, ubp_dtype dtype, void *stream);
+ubp_status launch_save(const CheckpointArgs &a, ubp_dtype dtype, void *stream);
+ubp_status launch_load(const CheckpointArgs &a, ubp_dtype dtype, void *stream);
 ubp_status launch_floor(void *stream);
 // The same kernels with the epilogue of ep.on == 2 (the sources compiled with UBP_WIDE).
 ubp_status launch_wros_wide(const ubp_packed *p, const void *X, int64_t ldx, int N, void *Y, int64_t ldy, ubp_dtype y_dtype,

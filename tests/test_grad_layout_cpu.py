@@ -1,0 +1,146 @@
+"""The weight gradient's layout on the host: every kept weight is the product of its own row of G and row of X, once, and
+what the kernel reads lies inside the arrays.  The builder is compiled with gcc and its sanitizers into a driver program."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+import paper_2407_19644_amd as ubp
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2407_19644_amd", "csrc")
+
+DRIVER = r"""
+#include <cstdio>
+#include <cstdlib>
+#include <vector>
+#include "ubp_internal.h"
+
+namespace ubp {
+ubp_status upload(ubp_packed *) { return UBP_ERR_DEVICE; }
+void release_device(ubp_packed *) {}
+}
+
+#define CHECK(c) do { if (!(c)) { std::fprintf(stderr, "line %d: %s\n", __LINE__, #c); return 1; } } while (0)
+
+int main(int argc, char **argv) {
+    CHECK(argc == 8);
+    const int M = atoi(argv[1]), K = atoi(argv[2]), bh = atoi(argv[3]), bw = atoi(argv[4]), mode = atoi(argv[6]);
+    const double density = atof(argv[5]);
+    const ubp_dtype dt = (ubp_dtype)atoi(argv[7]);
+    int64_t nb = ubp_target_block_count(M, K, bh, bw, density);
+    std::vector<ubp_block> blocks((size_t)nb + 1);
+    int64_t got = 0;
+    CHECK(ubp_select_reference(M, K, bh, bw, density, 7, mode, 1.1, blocks.data(), nb, &got) == UBP_OK && got == nb);
+    std::vector<unsigned char> W((size_t)M * K * (dt == UBP_F32 ? 4 : 2), 1);
+    ubp_packed *p = nullptr;
+    CHECK(ubp_pack(W.data(), dt, M, K, K, bh, bw, blocks.data(), nb, UBP_HOST_ONLY, &p) == UBP_OK);
+    const ubp::GradLayout &L = ubp::get_grad_layout(p);
+    CHECK(L.usable && L.built);
+    CHECK((int64_t)L.ops.size() == L.n_tiles * 16 && (int64_t)L.inv.size() == L.n_tiles * 256 && (int)L.regions.size() == 8 * L.n_regions);
+    CHECK(L.max_tiles <= ubp::kGradMaxTiles && L.max_slots <= ubp::kGradMaxSlots);
+    std::vector<int32_t> start((size_t)nb);
+    for (int r = 0; r + bh <= M; ++r)
+        for (int32_t b = p->indptr[(size_t)r]; b < p->indptr[(size_t)r + 1]; ++b) start[(size_t)b] = r;
+    std::vector<char> seen((size_t)(nb * bh * bw), 0);
+    int64_t next_tile = 0, next_row = 0;
+    for (int g = 0; g < L.n_regions; ++g) {
+        const int32_t *R = &L.regions[(size_t)g * 8];
+        const int64_t first = R[0], tiles = R[1], rows = R[2], g_slots = R[3], slots = R[4];
+        CHECK(first == next_tile && tiles >= 1 && rows == next_row);
+        next_tile += tiles;
+        next_row += slots;
+        CHECK(g_slots % 16 == 0 && slots % 16 == 0 && g_slots < slots && slots <= L.max_slots);
+        CHECK((tiles + ubp::kGradWaves - 1) / ubp::kGradWaves <= L.max_tiles);
+        for (int64_t s = 0; s < slots; ++s) {
+            const int32_t row = L.rows[(size_t)(rows + s)];
+            CHECK(row >= -1 && row < (s < g_slots ? M : K));
+        }
+        for (int64_t t = first; t < first + tiles; ++t) {
+            int32_t gr[16], xr[16];
+            for (int k = 0; k < 16; ++k) {
+                const uint32_t o = L.ops[(size_t)(t * 16 + k)];
+                CHECK((int64_t)(o & 0xffff) < g_slots && (int64_t)(o >> 16) >= g_slots && (int64_t)(o >> 16) < slots);
+                gr[k] = L.rows[(size_t)(rows + (o & 0xffff))];
+                xr[k] = L.rows[(size_t)(rows + (o >> 16))];
+            }
+            for (int i = 0; i < 16; ++i)
+                for (int j = 0; j < 16; ++j) {
+                    const int32_t v = L.inv[(size_t)(t * 256 + (16 * (i / 4) + j) * 4 + i % 4)];
+                    CHECK(v >= -1 && v < nb * bh * bw);
+                    if (v < 0) continue;
+                    CHECK(!seen[(size_t)v]);
+                    seen[(size_t)v] = 1;
+                    const int64_t b = v / (bh * bw);
+                    const int q = v / bh % bw, s = v % bh;
+                    const int row = start[(size_t)b] + ((s - start[(size_t)b]) % bh + bh) % bh;
+                    CHECK(gr[i] == row && xr[j] == p->indices[(size_t)b] + q);
+                }
+        }
+    }
+    CHECK(next_tile == L.n_tiles && next_row == (int64_t)L.rows.size());
+    for (char c : seen) CHECK(c);
+    for (int64_t steps : {0, 1, 3, 4, 7, 8, 31, 256, 392, 4096, 1 << 26}) {
+        const int64_t s = ubp::grad_splits(L, steps);
+        CHECK(s >= 1 && s <= 256 && (s == 1 || s * ubp::kGradMinSteps <= steps));
+    }
+    std::printf("%lld tiles %d regions %d of a wavefront %d rows\n", (long long)L.n_tiles, L.n_regions, L.max_tiles, L.max_slots);
+    ubp_packed_free(p);
+    return 0;
+}
+"""
+
+LAYERS = [  # M, K, bh, bw, density, mode, dtype
+    (64, 64, 4, 4, 0.5, 0, 0), (960, 160, 4, 4, 0.3, 0, 1), (256, 2304, 4, 4, 0.25, 0, 2), (512, 512, 4, 1, 0.2, 0, 1),
+    (1024, 1024, 16, 16, 0.1, 1, 2), (100, 300, 8, 8, 0.2, 0, 2), (70, 45, 3, 1, 0.4, 0, 0), (33, 40, 5, 3, 0.3, 0, 1),
+    (256, 256, 2, 1, 0.3, 0, 1), (256, 256, 1, 1, 0.5, 0, 1), (64, 900, 1, 7, 0.3, 0, 2), (130, 90, 20, 4, 0.3, 0, 1),
+    (300, 64, 33, 2, 0.2, 0, 0), (16, 16, 16, 16, 1.0, 0, 1), (40, 50, 40, 50, 1.0, 0, 2), (17, 19, 1, 1, 1.0, 0, 2),
+    (96, 3000, 2, 2, 0.9, 0, 2)[:4] + (0.5, 0, 2), (8, 8, 4, 4, 0.0, 0, 1), (1, 1, 1, 1, 1.0, 0, 0), (4096, 4096, 16, 16, 0.1, 1, 2),
+]
+
+
+@pytest.fixture(scope="module")
+def driver(tmp_path_factory):
+    gxx = shutil.which("g++")
+    if gxx is None:
+        pytest.skip("no g++")
+    d = tmp_path_factory.mktemp("grad_layout")
+    src = d / "driver.cpp"
+    src.write_text(DRIVER)
+    exe = d / "driver"
+    cmd = [gxx, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+           "-I", os.path.join(ROOT, "include"), "-I", CSRC, str(src)]
+    cmd += [os.path.join(CSRC, s) for s in ("ubp_host.cpp", "ubp_layouts.cpp", "ubp_grad_layout.cpp")] + ["-o", str(exe), "-lpthread"]
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert r.returncode == 0, r.stdout
+    return str(exe)
+
+
+@pytest.mark.parametrize("args", LAYERS, ids=lambda a: "x".join(map(str, a)))
+def test_layout(driver, args):
+    r = subprocess.run([driver] + [str(a) for a in args], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
+    print(r.stdout)
+    assert r.returncode == 0, r.stdout
+
+
+def test_refusals_without_a_device():
+    """A handle without a device: sizes of workspaces, and refused calls."""
+    import numpy as np
+    from layer_util import layer
+    blocks, W, _ = layer(64, 48, 4, 4, 0.3, "f16", 1)
+    p = ubp.pack(W, "f16", 4, 4, blocks)
+    assert ubp.weight_grad_workspace(p, 0) == 0 and ubp.weight_grad_workspace(p, 1) == 0
+    assert ubp.weight_grad_workspace(p, 100000) > 0 and ubp.weight_grad_workspace(p, 100000) % 1024 == 0
+    assert ubp.linear_grad_workspace(p, 8192) == 0 and ubp.linear_grad_workspace(p, 8193) == 64 * 2 * 4
+    for call in (lambda: ubp.weight_grad_workspace(p, -1), lambda: ubp.linear_grad_workspace(p, -1)):
+        with pytest.raises(ubp.UBPError):
+            call()
+    for call in (lambda: ubp.weight_grad(p, 64, 8, 64, 8, 8, 64), lambda: ubp.weight_grad_checkpoint(p, 64, 8, 64, 8, 64, 1, 8, 64),
+                 lambda: ubp.weight_grad_prepare(p), lambda: ubp.linear_grad(p, 64, 8, 64, 8, 8, 64, 8, activation="silu"),
+                 lambda: ubp.checkpoint_save(p, 64, 8, 8, 64, 8, 64, 1), lambda: ubp.checkpoint_load(p, 64, 8, 64, 1, 8, 64, 8)):
+        with pytest.raises(ubp.UBPError) as e:
+            call()
+        assert e.value.code == 1
+    with pytest.raises(KeyError):
+        ubp.linear_grad(p, 64, 8, 64, 8, 8, 64, 8, activation="swish")

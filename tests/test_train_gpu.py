@@ -1,0 +1,488 @@
+"""The backward pass of a pruned layer: gradient of the epilogue, inputs in 8 bits, weight gradient, and a whole step."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+import paper_2407_19644_amd as ubp                                      # noqa: E402
+from gpu_util import _TORCH, from_device, to_device                    # noqa: E402
+from layer_util import act, act_slope, checkpoint_of, half_step, layer, value_cells   # noqa: E402
+from synthetic import decode_f64, encode, make_activations, select_blocks             # noqa: E402
+
+DEV = "cuda"
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def handle(M, K, dtype, blocks=None, bh=1, bw=1):
+    W = encode(np.zeros((M, K), np.float32), dtype)
+    return ubp.pack(W, dtype, bh, bw, np.zeros((0, 2), np.int32) if blocks is None else blocks, device=torch.cuda.current_device())
+
+
+def pitched(enc, dtype, ld, off=0, fill=float("nan")):
+    """A device matrix with rows `ld` elements apart, beginning `off` elements behind an aligned address; what lies around it is
+    `fill`.  Returns (the view, everything)."""
+    M, N = enc.shape
+    t = torch.from_numpy(np.ascontiguousarray(enc))
+    t = t.view(torch.bfloat16) if dtype == "bf16" else t
+    buf = torch.full((M * ld + off + 64,), fill, dtype=t.dtype, device=DEV) if t.dtype.is_floating_point else \
+        torch.full((M * ld + off + 64,), int(fill), dtype=t.dtype, device=DEV)
+    view = buf[off:off + M * ld].view(M, ld)[:, :N]
+    view.copy_(t.cuda())
+    return view, buf
+
+
+def workspace(n):
+    """Exactly n bytes (16-byte aligned) between guards."""
+    buf = torch.full((n + 512,), 0xA5, dtype=torch.uint8, device=DEV)
+    return buf, buf.data_ptr() + 256
+
+
+def guards_intact(buf, n):
+    return bool((buf[:256] == 0xA5).all() and (buf[256 + n:] == 0xA5).all())
+
+
+# ------------------------------------------------------------------ gradient of the epilogue
+def run_linear_grad(p, dY, Z, dtype, activation, lo=0.0, hi=0.0, bias=True, ld=None, off=0, inplace=None):
+    M, N = dY.shape
+    ld = ld or N
+    d, dbuf = pitched(dY, dtype, ld, off)
+    z, zbuf = pitched(Z, dtype, ld, off)
+    g, gbuf = pitched(np.zeros_like(dY), dtype, ld, off)
+    if inplace == "dY":
+        g, gbuf = d, dbuf
+    if inplace == "Z":
+        g, gbuf = z, zbuf
+    db = torch.full((M,), float("nan"), device=DEV)
+    n = ubp.linear_grad_workspace(p, N)
+    ws, wp = workspace(n)
+    ubp.linear_grad(p, d.data_ptr(), ld, z.data_ptr(), ld, N, g.data_ptr(), ld, db.data_ptr() if bias else None, activation, lo, hi,
+                    wp, n, stream())
+    torch.cuda.synchronize()
+    assert guards_intact(ws, n)
+    around = gbuf.clone()
+    around[off:off + M * ld].view(M, ld)[:, :N] = float("nan")
+    assert torch.isnan(around.float()).all(), "wrote outside the matrix"
+    return from_device(g.contiguous(), dtype), db.cpu().numpy().astype(np.float64)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,N", [(1, 1), (3, 7), (5, 64), (4, 2047), (6, 2048), (9, 2049), (7, 8192), (3, 8193), (2, 20001), (1025, 2050), (1024, 33)])
+def test_linear_grad(M, N, dtype):
+    rng = np.random.default_rng(M * 31 + N)
+    dY = encode(rng.standard_normal((M, N)).astype(np.float32), dtype)
+    z = 2.0 * rng.standard_normal((M, N))
+    z[rng.random((M, N)) < 0.05] = 0.0
+    Z = encode(z.astype(np.float32), dtype)
+    d64, z64 = decode_f64(dY, dtype), decode_f64(Z, dtype)
+    p = handle(M, 8, dtype)
+    lo, hi = float(np.float32(-0.5)), float(np.float32(0.75))
+    z64.flat[0], d64.flat[0] = lo, 1.0
+    Z, dY = encode(z64.astype(np.float32), dtype), encode(d64.astype(np.float32), dtype)
+    for i, a in enumerate((None, "relu", "clamp", "gelu", "gelu_tanh", "silu")):
+        G, db = run_linear_grad(p, dY, Z, dtype, a, lo, hi, ld=N + (0, 1, 8, 3, 0, 16)[i], off=(0, 1, 8, 0, 5, 0)[i],
+                                inplace=(None, "dY", "Z", None, "dY", None)[i])
+        want = d64 * act_slope(a, z64, lo, hi)
+        # the slope: F + z F', both within 4e-7, and fp32 roundings of z and the product; then the rounding to the type
+        err = np.abs(d64) * (4e-7 + 2.0 ** -23 * (1 + np.abs(z64))) + 2.0 ** -24 * np.abs(want)
+        err = np.where(np.isin(a or "none", ("none", "relu", "clamp")), 0.0, err)
+        assert (np.abs(G - want) <= 1.01 * (err + half_step(np.abs(want) + err, dtype)) + 1e-37).all(), a
+        # sums of the values before they are rounded: a tree over chunks, below 64 additions deep on any path
+        tol = err.sum(1) + 64 * 2.0 ** -24 * np.abs(want).sum(1) + 1e-37
+        assert (np.abs(db - want.sum(1)) <= tol).all(), (a, float((np.abs(db - want.sum(1)) / tol).max()))
+    p.free()
+
+
+def test_linear_grad_without_bias_and_without_tokens():
+    p = handle(5, 8, "f16")
+    rng = np.random.default_rng(0)
+    dY = encode(rng.standard_normal((5, 100)).astype(np.float32), "f16")
+    G, db = run_linear_grad(p, dY, dY, "f16", "silu", bias=False)
+    assert np.isnan(db).all()
+    d = torch.full((5,), 7.0, device=DEV)
+    ubp.linear_grad(p, None, 0, None, 0, 0, None, 0, d.data_ptr(), "silu", stream=stream())
+    torch.cuda.synchronize()
+    assert (d == 0).all()
+    # the identity needs no Z
+    y, _ = pitched(dY, "f16", 100)
+    g = torch.empty_like(y)
+    ubp.linear_grad(p, y.data_ptr(), 100, None, 0, 100, g.data_ptr(), 100, d.data_ptr(), None, stream=stream())
+    torch.cuda.synchronize()
+    assert torch.equal(g, y)
+    p.free()
+
+
+def test_linear_grad_of_values_that_are_not_finite():
+    p = handle(2, 8, "f32")
+    Z = np.asarray([[np.nan, np.inf, -np.inf, 1e30, -1e30, 0.0, 1.0, -1.0]] * 2, np.float32)
+    dY = np.asarray([[2.0] * 8, [np.nan] * 8], np.float32)
+    for a in ("gelu", "gelu_tanh", "silu"):
+        G, _ = run_linear_grad(p, dY, Z, "f32", a)
+        assert np.isnan(G[0, 0]) and np.isnan(G[1]).all()
+        assert (G[0, 1:5] == [2.0, 0.0, 2.0, 0.0]).all()
+    for a, lo, hi, slope in (("relu", 0, 0, [0, 1, 0, 1, 0, 0, 1, 0]), ("clamp", -1.0, 1.0, [0, 0, 0, 0, 0, 1, 1, 1])):
+        G, _ = run_linear_grad(p, dY, Z, "f32", a, lo, hi)
+        assert (G[0] == 2.0 * np.asarray(slope)).all()
+        assert (np.isnan(G[1]) == (np.asarray(slope) == 1)).all() and (G[1][np.asarray(slope) == 0] == 0).all()
+    p.free()
+
+
+def test_linear_grad_against_differences():
+    """(act(z + h) - act(z - h)) / 2 h through the forward call, in fp32 at steps where both errors are about equal: h = 2^-7,
+    h^2 / 6 max|act'''| (2.2 for the three) = 2.2e-5, and 2 x 4e-7 |act| / 2 h = 5e-5 |z|."""
+    N = 401
+    z = np.linspace(-5, 5, N).astype(np.float32)
+    h = np.float32(2.0 ** -7)
+    W = np.eye(2, dtype=np.float32)
+    p = ubp.pack(W, "f32", 1, 1, np.asarray([[0, 0], [1, 1]], np.int32), device=torch.cuda.current_device())
+    X = np.stack([z + h, z - h])
+    for a in ("gelu", "gelu_tanh", "silu"):
+        x, y = to_device(X, "f32"), torch.empty((2, N), device=DEV)
+        ubp.linear(p, x.data_ptr(), N, N, y.data_ptr(), N, "f32", activation=a, stream=stream())
+        torch.cuda.synchronize()
+        y = y.cpu().numpy().astype(np.float64)
+        diff = (y[0] - y[1]) / (X[0].astype(np.float64) - X[1])
+        G, _ = run_linear_grad(p, np.ones((2, N), np.float32), np.stack([z, z]), "f32", a)
+        assert (np.abs(G[0] - diff) <= 2.5e-5 + 6e-5 * np.abs(z) + 1e-5).all()
+    p.free()
+
+
+# ------------------------------------------------------------------ inputs in 8 bits
+def special_values(K, N, dtype, seed):
+    """Normal rows of every size, rows of zeros, subnormals, values at the type's end, ties, Inf and NaN among them."""
+    rng = np.random.default_rng(seed)
+    X = rng.standard_normal((K, N)) * 2.0 ** rng.integers(-12, 12, (K, 1))
+    if K > 1:
+        X[1] = 0.0
+    if K > 2:
+        X[2] = np.float64(65504.0 if dtype == "f16" else 3.38e38) * rng.uniform(-1, 1, N)
+    if K > 3:
+        X[3] = 2.0 ** (-24 if dtype == "f16" else -133) * rng.integers(-9, 9, N)
+    if K > 4:
+        X[4] = (rng.integers(0, 128, N) * 0.125 + 8) * np.where(rng.random(N) < 0.5, -1, 1)     # ties between codes
+        X[4, ::32] = 448.0
+    if K > 5:
+        X[5, rng.random(N) < 0.1] = np.inf
+        X[5, rng.random(N) < 0.1] = -np.inf
+        X[5, rng.random(N) < 0.1] = np.nan
+    if K > 6:
+        X[6] = np.nan
+    if K > 7:
+        X[7] = -0.0
+        X[7, N // 2] = 1.75 * 2.0 ** 3
+    with np.errstate(over="ignore"):
+        return np.clip(X, -65504, 65504).astype(np.float32) if dtype == "f16" else X.astype(np.float32)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("K,N,pad,off", [(9, 1, 0, 0), (9, 31, 3, 1), (9, 32, 0, 0), (10, 33, 7, 3), (9, 160, 0, 8), (12, 1023, 0, 0), (9, 1024, 1, 0),
+                                         (17, 1025, 0, 5), (8, 4096, 0, 0)])
+def test_checkpoint(K, N, pad, off, dtype):
+    x = special_values(K, N, dtype, K + N)
+    if dtype == "bf16":
+        fin = np.isfinite(x)
+        X = np.where(fin, encode(np.where(fin, x, 0), "bf16"), np.where(np.isnan(x), 0x7fc0, np.where(x > 0, 0x7f80, 0xff80))).astype(np.uint16)
+    else:
+        X = encode(x, dtype) if dtype == "f32" else x.astype(np.float16)
+    X64 = decode_f64(X, dtype)
+    codes, exps, vals = checkpoint_of(X64, dtype)
+    p = handle(4, K, dtype)
+    G = (N + 31) // 32
+    xv, _ = pitched(X, dtype, N + pad, off)
+    q, qbuf = pitched(np.zeros((K, N), np.uint8), "u8", N + pad, off, fill=0x5A)
+    s, sbuf = pitched(np.zeros((K, G), np.uint8), "u8", G + pad, off, fill=0x5A)
+    ubp.checkpoint_save(p, xv.data_ptr(), N + pad, N, q.data_ptr(), N + pad, s.data_ptr(), G + pad, stream())
+    out, obuf = pitched(X, dtype, N + pad, off)
+    out.fill_(3.0)
+    ubp.checkpoint_load(p, q.data_ptr(), N + pad, s.data_ptr(), G + pad, N, out.data_ptr(), N + pad, stream())
+    torch.cuda.synchronize()
+    got_q, got_s, got = q.cpu().numpy(), s.cpu().numpy(), from_device(out.contiguous(), dtype)
+    assert np.array_equal(got_s, exps)
+    nan = (codes & 127) == 127
+    assert np.array_equal(got_q[~nan], codes[~nan]) and ((got_q[nan] & 127) == 127).all()
+    want = decode_f64(encode(np.where(nan, 0, vals).astype(np.float32), dtype), dtype)
+    assert np.array_equal(got[~nan], want[~nan]) and np.isnan(got[nan]).all() and np.isfinite(got[~nan]).all()
+    assert np.array_equal(np.signbit(got[~nan]), np.signbit(X64[~nan]))
+    # the promised distance
+    fin = np.isfinite(X64)
+    step = 2.0 ** (np.repeat(exps.astype(np.float64) - 127, 32, axis=1)[:, :N] - 10)
+    assert (np.abs(vals - X64)[fin] <= np.maximum(2.0 ** -4 * np.abs(X64), step)[fin]).all()
+    for buf, view, rows, width in ((qbuf, q, K, N), (sbuf, s, K, G)):
+        around = buf.clone()
+        around[off:off + rows * (width + pad)].view(rows, width + pad)[:, :width] = 0x5A
+        assert (around == 0x5A).all()
+    around = obuf.clone()
+    around[off:off + K * (N + pad)].view(K, N + pad)[:, :N] = float("nan")
+    assert torch.isnan(around.float()).all()
+    p.free()
+
+
+# ------------------------------------------------------------------ weight gradient
+def run_weight_grad(p, G, X, dtype, n_values, ckpt=None, ldg=None, ldx=None, off=0, accumulate=False, init=None, repeat=1):
+    """dvalues as float64.  ckpt: (codes, exponent bytes) in the place of X."""
+    N = G.shape[1]
+    g, _ = pitched(G, dtype, ldg or N, off)
+    out = torch.full((n_values + 8,), float("nan"), device=DEV)
+    if init is not None:
+        out[:n_values] = torch.from_numpy(init).cuda()
+    n = ubp.weight_grad_workspace(p, N)
+    ws, wp = workspace(n)
+    if ckpt is None:
+        x, _ = pitched(X, dtype, ldx or N, off)
+    else:
+        x, _ = pitched(ckpt[0], "u8", ldx or N, off, fill=0x7f)
+        s, _ = pitched(ckpt[1], "u8", ckpt[1].shape[1] + 3, off, fill=0xff)
+    for _ in range(repeat):
+        if ckpt is None:
+            ubp.weight_grad(p, g.data_ptr(), ldg or N, x.data_ptr(), ldx or N, N, out.data_ptr(), accumulate, wp, n, stream())
+        else:
+            ubp.weight_grad_checkpoint(p, g.data_ptr(), ldg or N, x.data_ptr(), ldx or N, s.data_ptr(), ckpt[1].shape[1] + 3, N, out.data_ptr(),
+                                       accumulate, wp, n, stream())
+    torch.cuda.synchronize()
+    assert guards_intact(ws, n)
+    assert torch.isnan(out[n_values:]).all()
+    return out[:n_values].cpu().numpy().astype(np.float64)
+
+
+def weight_tolerance(G64, X64, rows, cols, N):
+    """n products summed in fp32, in any order: n 2^-24 of the sum of magnitudes; twice that where a matrix instruction rounds its
+    partial sums on the way; and the ranges' sums."""
+    mag = (np.abs(G64) @ np.abs(X64).T)[rows, cols]
+    return 2.0 * (min(N, 1 << 16) + 260) * 2.0 ** -24 * mag + 1e-37
+
+
+GRAD_CASES = [  # M, K, N, bh, bw, density, dtype
+    (64, 64, 196, 4, 4, 0.5, "f32"), (70, 45, 67, 3, 1, 0.4, "f32"), (300, 130, 1000, 16, 16, 0.2, "f32"),
+    (960, 160, 1567, 4, 4, 0.3, "f16"), (33, 40, 1, 5, 3, 0.3, "f16"), (130, 90, 35, 20, 4, 0.3, "f16"), (200, 256, 328, 8, 8, 0.2, "f16"),
+    (256, 600, 4096, 4, 4, 0.25, "bf16"), (130, 600, 1001, 16, 16, 0.15, "bf16"), (40, 50, 17, 40, 50, 1.0, "bf16"),
+    (16, 16, 32, 16, 16, 1.0, "bf16"), (1, 1, 5, 1, 1, 1.0, "bf16"), (512, 512, 64, 4, 1, 0.2, "bf16"), (700, 800, 300, 2, 3, 0.3, "bf16"),
+    (2048, 1024, 520, 16, 16, 0.15, "bf16"), (1500, 1400, 40, 16, 16, 0.2, "f32"),
+]
+
+
+@pytest.mark.parametrize("case", GRAD_CASES, ids=lambda c: "-".join(map(str, c)))
+def test_weight_grad(case):
+    M, K, N, bh, bw, d, dtype = case
+    blocks = select_blocks(M, K, bh, bw, d, seed=M + K)
+    rows, cols = value_cells(blocks, bh, bw)
+    G = make_activations(M, N, M + 1, dtype, "normal")
+    X = make_activations(K, N, K + 2, dtype, "normal")
+    G64, X64 = decode_f64(G, dtype), decode_f64(X, dtype)
+    p = handle(M, K, dtype, blocks, bh, bw)
+    want = (G64 @ X64.T)[rows, cols]
+    tol = weight_tolerance(G64, X64, rows, cols, N)
+    got = run_weight_grad(p, G, X, dtype, rows.size)
+    assert (np.abs(got - want) <= tol).all(), float((np.abs(got - want) / tol).max())
+    # other pitches and alignments: the same sums in the same order
+    for ldg, ldx, off in ((N + 1, N + 3, 1), (N + 8, N + 16, 8), (N + 5, N, 3)):
+        assert np.array_equal(run_weight_grad(p, G, X, dtype, rows.size, ldg=ldg, ldx=ldx, off=off), got)
+    # added to what is there
+    init = np.linspace(-3, 3, rows.size).astype(np.float32)
+    acc = run_weight_grad(p, G, X, dtype, rows.size, accumulate=True, init=init, repeat=2)
+    assert (np.abs(acc - (init + 2 * want)) <= 2 * tol + 2.0 ** -22 * (np.abs(init) + 2 * np.abs(want))).all()
+    # from a checkpoint: what the loaded values give, bit for bit
+    codes, exps, vals = checkpoint_of(X64, dtype)
+    X8 = encode(vals.astype(np.float32), dtype)
+    got8 = run_weight_grad(p, G, None, dtype, rows.size, ckpt=(codes, exps))
+    assert np.array_equal(got8, run_weight_grad(p, G, X8, dtype, rows.size))
+    assert np.array_equal(got8, run_weight_grad(p, G, None, dtype, rows.size, ckpt=(codes, exps), ldg=N + 3, ldx=N + 5, off=7))
+    want8 = (G64 @ decode_f64(X8, dtype).T)[rows, cols]
+    assert (np.abs(got8 - want8) <= tol * 2).all()
+    p.free()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_weight_grad_of_whole_numbers_is_exact(dtype):
+    """Small whole numbers: every sum is exact in fp32, in any order."""
+    M, K, N, bh, bw = 200, 300, 777, 4, 4
+    blocks = select_blocks(M, K, bh, bw, 0.3, seed=3)
+    rows, cols = value_cells(blocks, bh, bw)
+    rng = np.random.default_rng(1)
+    G64, X64 = rng.integers(-8, 9, (M, N)).astype(np.float64), rng.integers(-8, 9, (K, N)).astype(np.float64)
+    p = handle(M, K, dtype, blocks, bh, bw)
+    got = run_weight_grad(p, encode(G64.astype(np.float32), dtype), encode(X64.astype(np.float32), dtype), dtype, rows.size)
+    assert np.array_equal(got, (G64 @ X64.T)[rows, cols])
+    p.free()
+
+
+def test_weight_grad_of_nothing():
+    blocks = select_blocks(64, 64, 4, 4, 0.3, seed=3)
+    n = blocks.shape[0] * 16
+    p = handle(64, 64, "bf16", blocks, 4, 4)
+    out = torch.full((n,), 5.0, device=DEV)
+    ubp.weight_grad(p, None, 0, None, 0, 0, out.data_ptr(), True, stream=stream())
+    torch.cuda.synchronize()
+    assert (out == 5.0).all()
+    ubp.weight_grad_checkpoint(p, None, 0, None, 0, None, 0, 0, out.data_ptr(), stream=stream())
+    torch.cuda.synchronize()
+    assert (out == 0.0).all()
+    p.free()
+    empty = handle(64, 64, "bf16")
+    ubp.weight_grad(empty, None, 0, None, 0, 8, None, stream=stream())
+    assert ubp.weight_grad_workspace(empty, 4096) == 0
+    ubp.weight_grad_prepare(empty)
+    empty.free()
+
+
+def test_weight_grad_keeps_not_finite_values_in_their_rows():
+    M, K, N = 64, 96, 200
+    blocks = select_blocks(M, K, 8, 8, 0.4, seed=5)
+    rows, cols = value_cells(blocks, 8, 8)
+    G = decode_f64(make_activations(M, N, 1, "bf16", "normal"), "bf16")
+    X = decode_f64(make_activations(K, N, 2, "bf16", "normal"), "bf16")
+    G[5, 7], X[11, 199] = np.nan, np.inf
+    p = handle(M, K, "bf16", blocks, 8, 8)
+
+    def enc(a):
+        fin = np.isfinite(a)
+        return np.where(fin, encode(np.where(fin, a, 0).astype(np.float32), "bf16"), np.where(np.isnan(a), 0x7fc0, 0x7f80)).astype(np.uint16)
+
+    got = run_weight_grad(p, enc(G), enc(X), "bf16", rows.size)
+    touched = (rows == 5) | (cols == 11)
+    assert touched.any() and np.isfinite(got[~touched]).all() and not np.isfinite(got[touched]).any()
+    p.free()
+
+
+def test_refusals():
+    M, K, N = 64, 64, 20000
+    blocks = select_blocks(M, K, 4, 4, 0.3, seed=3)
+    p = handle(M, K, "f16", blocks, 4, 4)
+    G = torch.zeros((M, N), dtype=torch.float16, device=DEV)
+    X = torch.zeros((K, N), dtype=torch.float16, device=DEV)
+    Q = torch.zeros((K, N), dtype=torch.uint8, device=DEV)
+    S = torch.zeros((K, N // 32), dtype=torch.uint8, device=DEV)
+    out = torch.full((blocks.shape[0] * 16,), 7.0, device=DEV)
+    db = torch.full((M,), 7.0, device=DEV)
+    n = ubp.weight_grad_workspace(p, N)
+    nl = ubp.linear_grad_workspace(p, N)
+    assert n > 0 and nl > 0
+    ws = torch.empty(max(n, nl) + 16, dtype=torch.uint8, device=DEV)
+    g, x, q, s, o, w, b = (t.data_ptr() for t in (G, X, Q, S, out, ws, db))
+    wg, wc, lg, sv, ld = ubp.weight_grad, ubp.weight_grad_checkpoint, ubp.linear_grad, ubp.checkpoint_save, ubp.checkpoint_load
+    for call in (lambda: wg(p, None, N, x, N, N, o, False, w, n), lambda: wg(p, g, N, None, N, N, o, False, w, n),
+                 lambda: wg(p, g, N, x, N, N, None, False, w, n), lambda: wg(p, g, N - 1, x, N, N, o, False, w, n),
+                 lambda: wg(p, g, N, x, N - 1, N, o, False, w, n), lambda: wg(p, g, N, x, N, -1, o, False, w, n),
+                 lambda: wg(p, g, N, x, N, N, o, False, None, n), lambda: wg(p, g, N, x, N, N, o, False, w, n - 1),
+                 lambda: wg(p, g, N, x, N, N, o, False, w + 8, n), lambda: wc(p, g, N, q, N, None, N // 32, N, o, False, w, n),
+                 lambda: wc(p, g, N, q, N, s, N // 32 - 1, N, o, False, w, n), lambda: wc(p, g, N, None, N, s, N // 32, N, o, False, w, n),
+                 lambda: lg(p, None, N, x, N, N, g, N, b, "silu", 0, 0, w, nl), lambda: lg(p, x, N, None, N, N, g, N, b, "silu", 0, 0, w, nl),
+                 lambda: lg(p, x, N, x, N, N, None, N, b, "silu", 0, 0, w, nl), lambda: lg(p, x, N, x, N - 1, N, g, N, b, "silu", 0, 0, w, nl),
+                 lambda: lg(p, x, N, x, N, N, g, N, b, "silu", 0, 0, None, 0), lambda: lg(p, x, N, x, N, N, g, N, b, "silu", 0, 0, w, nl - 1),
+                 lambda: lg(p, x, N, x, N, N, g, N, b, "silu", 0, 0, w + 4, nl), lambda: lg(p, x, N, x, N, N, g, N, b, "clamp", 1, 0, w, nl),
+                 lambda: sv(p, None, N, N, q, N, s, N // 32), lambda: sv(p, x, N, N, q, N - 1, s, N // 32),
+                 lambda: sv(p, x, N, N, q, N, s, N // 32 - 1), lambda: ld(p, q, N, None, N // 32, N, x, N), lambda: ld(p, q, N, s, N // 32, N, x, N - 1)):
+        with pytest.raises(ubp.UBPError) as e:
+            call()
+        assert e.value.code == 1
+    torch.cuda.synchronize()
+    assert (out == 7.0).all() and (db == 7.0).all()
+    p.free()
+
+
+# ------------------------------------------------------------------ a step
+def test_training_step():
+    """Forward, checkpoint, backward of one layer as a program runs them, captured into a graph on a stream of its own and
+    replayed on new inputs; every gradient against float64 from the checkpoint's values."""
+    M, K, N, bh, bw, dtype, a = 96, 200, 300, 8, 4, "bf16", "gelu"
+    blocks, W, Wd = layer(M, K, bh, bw, 0.25, dtype, seed=12)
+    rows, cols = value_cells(blocks, bh, bw)
+    p = ubp.pack(W, dtype, bh, bw, blocks, device=torch.cuda.current_device())
+    pt = ubp.pack(np.ascontiguousarray(W.T), dtype, bw, bh, blocks[:, ::-1], device=torch.cuda.current_device())
+    t, G32 = torch.bfloat16, (N + 31) // 32
+    new = lambda *s, d=t: torch.zeros(s, dtype=d, device=DEV)              # noqa: E731
+    X, R, Y, Xh, Z, dY, Gr, dX = new(K, N), new(M, N), new(M, N), new(K, N), new(M, N), new(M, N), new(M, N), new(K, N)
+    Q, S = new(K, N, d=torch.uint8), new(K, G32, d=torch.uint8)
+    b, db, dW = new(M, d=torch.float32), new(M, d=torch.float32), new(rows.size, d=torch.float32)
+    n = ubp.weight_grad_workspace(p, N)
+    ws = new(n + 16, d=torch.uint8)
+    ubp.spmm_prepare(p, X.data_ptr(), N, N, Y.data_ptr(), N, dtype)
+    ubp.spmm_prepare(pt, Gr.data_ptr(), N, N, dX.data_ptr(), N, dtype)
+    ubp.weight_grad_prepare(p)
+
+    def step():
+        st = stream()
+        ubp.linear(p, X.data_ptr(), N, N, Y.data_ptr(), N, dtype, b.data_ptr(), a, residual_ptr=R.data_ptr(), ldr=N, stream=st)
+        ubp.checkpoint_save(p, X.data_ptr(), N, N, Q.data_ptr(), N, S.data_ptr(), G32, st)
+        ubp.checkpoint_load(p, Q.data_ptr(), N, S.data_ptr(), G32, N, Xh.data_ptr(), N, st)
+        ubp.spmm_fused(p, Xh.data_ptr(), N, N, Z.data_ptr(), N, dtype, b.data_ptr(), stream=st)
+        ubp.linear_grad(p, dY.data_ptr(), N, Z.data_ptr(), N, N, Gr.data_ptr(), N, db.data_ptr(), a, stream=st)
+        ubp.weight_grad_checkpoint(p, Gr.data_ptr(), N, Q.data_ptr(), N, S.data_ptr(), G32, N, dW.data_ptr(), False, ws.data_ptr(), n, st)
+        ubp.spmm(pt, Gr.data_ptr(), N, N, dX.data_ptr(), N, dtype, st)
+
+    def load(seed):
+        for i, m in enumerate((X, R, dY)):
+            m.copy_(to_device(make_activations(m.shape[0], N, seed + i, dtype, "normal"), dtype))
+        b.copy_(torch.linspace(-1, 1 + seed % 3, M))
+
+    load(1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        side.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            step()
+    for seed in (10, 20, 30):
+        load(seed)
+        for m in (Y, Xh, Z, Gr, dX, Q, S, db, dW):
+            m.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        got = [m.clone() for m in (Y, Xh, Z, Gr, dX, db, dW)]
+        with torch.cuda.stream(side):
+            step()
+        torch.cuda.synchronize()
+        for u, v in zip(got, (Y, Xh, Z, Gr, dX, db, dW)):
+            assert torch.equal(u, v)
+        x64, r64, y64, dy64, xh64, z64, g64 = (from_device(m, dtype) for m in (X, R, Y, dY, Xh, Z, Gr))
+        b64 = b.cpu().numpy().astype(np.float64)[:, None]
+        assert np.array_equal(xh64, checkpoint_of(x64, dtype)[2])
+        near = lambda u, v, w: (np.abs(u - v) <= half_step(v, dtype) * 1.01 + w).all()      # noqa: E731
+        e = 4e-6 * (np.abs(Wd) @ np.abs(x64) + 1)                           # fp32 sums of up to 100 products, slope 1.13
+        assert near(y64, act(a, Wd @ x64 + b64) + r64, e)
+        assert near(z64, Wd @ xh64 + b64, e + 4e-6 * (np.abs(Wd) @ np.abs(xh64)))
+        assert near(g64, dy64 * act_slope(a, z64), 2e-6 * np.abs(dy64) * (1 + np.abs(z64)))
+        want_db = (dy64 * act_slope(a, z64)).sum(1)
+        assert (np.abs(db.cpu().numpy() - want_db) <= 5e-6 * np.abs(dy64).sum(1)).all()
+        assert (np.abs(dW.cpu().numpy() - (g64 @ xh64.T)[rows, cols]) <= weight_tolerance(g64, xh64, rows, cols, N)).all()
+        assert near(from_device(dX, dtype), Wd.T @ g64, 4e-6 * (np.abs(Wd.T) @ np.abs(g64)))
+    p.free()
+    pt.free()
+
+
+def test_gradients_against_differences():
+    """d/dW and d/db of sum(dY * act(W X + b)) by central differences of the float64 loss, at some kept weights: the chain
+    linear_grad -> weight_grad in fp32 (relative 2e-5: sums of 300 products, slopes within 1e-6, differences h^2)."""
+    M, K, N, bh, bw = 24, 40, 300, 4, 2
+    blocks, W, Wd = layer(M, K, bh, bw, 0.3, "f32", seed=2)
+    rows, cols = value_cells(blocks, bh, bw)
+    X, dY = make_activations(K, N, 1, "f32", "normal"), make_activations(M, N, 2, "f32", "normal")
+    b = np.linspace(-0.5, 0.5, M).astype(np.float32)
+    p = ubp.pack(W, "f32", bh, bw, blocks, device=torch.cuda.current_device())
+    x, d, bd = to_device(X, "f32"), to_device(dY, "f32"), torch.from_numpy(b).cuda()
+    z, g, db = torch.empty((M, N), device=DEV), torch.empty((M, N), device=DEV), torch.empty(M, device=DEV)
+    for a in ("gelu", "gelu_tanh", "silu"):
+        ubp.spmm_fused(p, x.data_ptr(), N, N, z.data_ptr(), N, "f32", bd.data_ptr(), stream=stream())
+        ubp.linear_grad(p, d.data_ptr(), N, z.data_ptr(), N, N, g.data_ptr(), N, db.data_ptr(), a, stream=stream())
+        torch.cuda.synchronize()
+        dv = run_weight_grad(p, g.cpu().numpy(), X, "f32", rows.size)
+        f = lambda w, bb: (dY.astype(np.float64) * act(a, w @ X.astype(np.float64) + bb[:, None])).sum()    # noqa: E731
+        h = 1e-4
+        scale = np.abs(dv).max()
+        for v in range(0, rows.size, max(1, rows.size // 25)):
+            up, down = Wd.copy(), Wd.copy()
+            up[rows[v], cols[v]] += h
+            down[rows[v], cols[v]] -= h
+            diff = (f(up, b.astype(np.float64)) - f(down, b.astype(np.float64))) / (2 * h)
+            assert abs(dv[v] - diff) <= 2e-5 * scale
+        for i in range(0, M, 5):
+            e = np.zeros(M)
+            e[i] = h
+            diff = (f(Wd, b + e) - f(Wd, b - e)) / (2 * h)
+            assert abs(db.cpu().numpy()[i] - diff) <= 2e-5 * np.abs(db.cpu().numpy()).max()
+    p.free()
