@@ -633,8 +633,8 @@ ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const vo
     a.out = dvalues;
     a.accumulate = accumulate ? 1 : 0;
     if (dry) {
-        ubp_status rc = launch_weight_grad(a, p->dtype, false, L->max_tiles, stream, true);
-        if (rc == UBP_OK) rc = launch_weight_grad(a, p->dtype, true, L->max_tiles, stream, true);
+        ubp_status rc = launch_weight_grad(a, p->dtype, false, L->shape, stream, true);
+        if (rc == UBP_OK) rc = launch_weight_grad(a, p->dtype, true, L->shape, stream, true);
         return rc;
     }
     if (N == 0) {
@@ -648,7 +648,7 @@ ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const vo
         if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0 || workspace_bytes < a.splits * L->n_tiles * 1024) return UBP_ERR_INVALID_ARG;
         a.part = static_cast<float *>(workspace);
     }
-    const ubp_status rc = launch_weight_grad(a, p->dtype, saved, L->max_tiles, stream, false);
+    const ubp_status rc = launch_weight_grad(a, p->dtype, saved, L->shape, stream, false);
     if (rc != UBP_OK || a.splits == 1) return rc;
     return launch_weight_sum(a, stream);
 } catch (const std::bad_alloc &) {

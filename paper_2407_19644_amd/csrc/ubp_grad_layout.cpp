@@ -34,9 +34,13 @@ void union_of(const std::vector<Tile> &tiles, const int32_t *order, int64_t n, s
 
 int64_t padded(size_t n) { return ((int64_t)n + 15) / 16 * 16; }
 
+struct Rows {
+    int64_t g, x; // LDS rows
+    int64_t all() const { return g + x; }
+};
 struct Region {
     int64_t first, n; // run of the tile order
-    int64_t slots;    // LDS rows
+    Rows rows;
 };
 
 } // namespace
@@ -121,9 +125,14 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
     std::vector<int32_t> g, x, by_row, by_col;
     auto slots = [&](const int32_t *o, int64_t count) {
         union_of(tiles, o, count, g, x);
-        return padded(g.size()) + padded(x.size());
+        return Rows{padded(g.size()), padded(x.size())};
     };
     if (n) open.push_back({0, n, slots(order.data(), n)});
+    auto rows_fit = [](const Rows &r) { return r.g <= kGradLargest.g_slots && r.x <= kGradLargest.x_slots; };
+    // (halves that need not be cut again for their rows come first)
+    auto cost = [&](const Rows (&h)[2]) {
+        return h[0].all() + h[1].all() + (rows_fit(h[0]) ? 0 : int64_t(1) << 40) + (rows_fit(h[1]) ? 0 : int64_t(1) << 40);
+    };
     // the workgroups of a split of the tokens are as many as an XCD has CUs, while a wavefront keeps two tiles at least
     const int64_t wanted = std::min<int64_t>(kGradRegions, (n + 2 * kGradWaves - 1) / (2 * kGradWaves));
     while (!open.empty()) {
@@ -132,7 +141,7 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
         for (size_t k = 1; k < open.size(); ++k)
             if (open[k].n > open[at].n) at = k;
         const Region r = open[at];
-        const bool fits = r.n <= (int64_t)kGradWaves * kGradMaxTiles && r.slots <= kGradMaxSlots;
+        const bool fits = r.n <= (int64_t)kGradWaves * kGradLargest.tiles && rows_fit(r.rows);
         if ((fits && (int64_t)(open.size() + done.size()) >= wanted) || r.n == 1) {
             done.push_back(r);
             open.erase(open.begin() + (ptrdiff_t)at);
@@ -151,9 +160,9 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
             return s.col[0] != t.col[0] ? s.col[0] < t.col[0] : s.r0 < t.r0;
         });
         const int64_t half = (r.n + 1) / 2;
-        const int64_t rows[2] = {slots(by_row.data(), half), slots(by_row.data() + half, r.n - half)};
-        const int64_t cs[2] = {slots(by_col.data(), half), slots(by_col.data() + half, r.n - half)};
-        const bool rows_win = rows[0] + rows[1] <= cs[0] + cs[1];
+        const Rows rows[2] = {slots(by_row.data(), half), slots(by_row.data() + half, r.n - half)};
+        const Rows cs[2] = {slots(by_col.data(), half), slots(by_col.data() + half, r.n - half)};
+        const bool rows_win = cost(rows) <= cost(cs);
         std::copy(rows_win ? by_row.begin() : by_col.begin(), rows_win ? by_row.end() : by_col.end(), o);
         open[at] = {r.first, half, rows_win ? rows[0] : cs[0]};
         open.push_back({r.first + half, r.n - half, rows_win ? rows[1] : cs[1]});
@@ -172,11 +181,11 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
         union_of(tiles, o, r.n, g, x);
         const int32_t first_slot = (int32_t)out.rows.size();
         const int32_t g_slots = (int32_t)padded(g.size()), all = g_slots + (int32_t)padded(x.size());
-        for (int32_t v : g) out.rows.push_back(v < p->M ? v : -1);
-        out.rows.resize((size_t)first_slot + (size_t)g_slots, -1);
+        for (int32_t v : g) out.rows.push_back(std::min(v, p->M - 1));
+        out.rows.resize((size_t)first_slot + (size_t)g_slots, out.rows.back());
         for (size_t k = 0; k < x.size(); ++k) slot_x[(size_t)x[k]] = g_slots + (int32_t)k;
         out.rows.insert(out.rows.end(), x.begin(), x.end());
-        out.rows.resize((size_t)first_slot + (size_t)all, -1);
+        out.rows.resize((size_t)first_slot + (size_t)all, out.rows.back());
         for (int64_t t = 0; t < r.n; ++t) {
             const Tile &a = tiles[(size_t)o[t]];
             const int64_t to = r.first + t;
@@ -187,8 +196,12 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
         }
         out.regions.insert(out.regions.end(), {(int32_t)r.first, (int32_t)r.n, first_slot, g_slots, all, 0, 0, 0});
         out.max_tiles = std::max(out.max_tiles, (int)((r.n + kGradWaves - 1) / kGradWaves));
+        out.max_g = std::max(out.max_g, (int)g_slots);
+        out.max_x = std::max(out.max_x, (int)(all - g_slots));
         out.max_slots = std::max(out.max_slots, (int)all);
     }
+    while (out.max_tiles > kGradShapes[out.shape].tiles || out.max_g > kGradShapes[out.shape].g_slots || out.max_x > kGradShapes[out.shape].x_slots)
+        ++out.shape; // (the largest holds them)
     out.n_regions = (int)done.size();
     L = std::move(out);
     return L;

@@ -215,20 +215,25 @@ struct Wros4Layout {
     std::vector<int32_t> rec_of_row, rec_of_end, row_of_rec;
 };
 
-// Weight gradient: wavefronts of a workgroup, tiles a wavefront keeps at most, LDS rows (of 64 bytes, two buffers) of a
-// region at most, regions that a layer is cut into where its tiles allow, workgroups that fill the card, steps of a range of
-// tokens at least.
+// Weight gradient: wavefronts of a workgroup, regions that a layer is cut into where its tiles allow, workgroups that fill
+// the card, steps of a range of tokens at least.
 constexpr int kGradWaves = 8;
-constexpr int kGradMaxTiles = 28;
-constexpr int kGradMaxSlots = 1264;
 constexpr int kGradRegions = 32;
 constexpr int kGradWorkgroups = 256;
 constexpr int kGradMinSteps = 4;
 
+// Tiles a wavefront keeps, LDS rows (of 64 bytes, in two buffers) for G and for X of a region, at most, per instantiation of
+// the kernel.
+struct GradShape { int tiles, g_slots, x_slots; };
+constexpr int kNumGradShapes = 4;
+constexpr GradShape kGradShapes[kNumGradShapes] = {{2, 256, 256}, {4, 256, 256}, {8, 384, 384}, {16, 640, 640}};
+constexpr GradShape kGradLargest = kGradShapes[kNumGradShapes - 1];
+static_assert((kGradLargest.g_slots + kGradLargest.x_slots) * 128 <= 160 * 1024, "two buffers fit LDS");
+
 // Host image of the weight gradient's layout.  A tile is the product of 16 consecutive rows of G with 16 rows of X; a region
 // is a run of tiles that one workgroup keeps in registers, with the rows of G and X that they need.
 //   regions : 8 words each: first tile, tiles, first entry of rows, entries for G (a multiple of 16), for G and X (likewise)
-//   rows    : row of G, then of X, per LDS row of the region; -1 for one that holds zeros
+//   rows    : row of G, then of X, per LDS row of the region (rows that fill up 16 repeat the last one)
 //   ops     : 16 words per tile: LDS row of G | LDS row of X << 16
 //   inv     : 256 words per tile: the value that element (16 (i / 4) + j) 4 + i % 4, row i and column j of the tile,
 //             is the gradient of (a place in the canonical values), -1 for none.  Every value appears once.
@@ -236,8 +241,9 @@ struct GradLayout {
     bool built = false, usable = false;
     int64_t n_tiles = 0;
     int n_regions = 0;
-    int max_tiles = 0; // of a wavefront
-    int max_slots = 0; // LDS rows of a region
+    int max_tiles = 0;                   // of a wavefront
+    int max_g = 0, max_x = 0, max_slots = 0; // LDS rows of a region
+    int shape = 0;                       // the smallest of kGradShapes that holds them
     std::vector<int32_t> regions, rows, inv;
     std::vector<uint32_t> ops;
 };
@@ -535,7 +541,7 @@ struct MtileShape { int rows, pixels, per_cu; };
 constexpr int kNumMtileShapes = 5;
 constexpr MtileShape kMtileShapes[kNumMtileShapes] = {{128, 128, 1}, {128, 64, 1}, {64, 128, 1}, {64, 64, 2}, {128, 256, 1}};
 ubp_status launch_mtile(const TileArgs &a, bool bf16, bool y_f32, int shape, int rows, void *stream, bool dry);
-ubp_status launch_weight_grad(const GradArgs &a, ubp_dtype dtype, bool checkpoint, int max_tiles, void *stream, bool dry);
+ubp_status launch_weight_grad(const GradArgs &a, ubp_dtype dtype, bool checkpoint, int shape, void *stream, bool dry);
 ubp_status launch_weight_sum(const GradArgs &a, void *stream);
 ubp_status launch_act_grad(const ActGradArgs &a, ubp_dtype dtype, void *stream);
 ubp_status launch_save(const CheckpointArgs &a, ubp_dtype dtype, void *stream);

@@ -33,16 +33,22 @@ template <> __device__ __forceinline__ float4v product<float>(uint4v a, uint4v b
 // One workgroup = one region (at most 8 T tiles of 16 rows of G x 16 rows of X) and one range of tokens.  Both operands of
 // the matrix instruction have the tokens along their inner dimension, as G and X have them in memory, so that a tile may
 // pair any rows: nothing is transposed, and only tiles that keep weights are formed.
-//  * A step = 64 bytes of every row that the region needs, through registers into one of two LDS buffers (the next step's
-//    loads are in flight while this one is multiplied), 16 bytes per lane.
-//  * A tile reads 1 KB of each operand from LDS per step, and its sums stay in a wavefront's registers for the whole range.
+//  * A step = 64 bytes of every row that the region needs, through registers into one of two LDS buffers: the next step's
+//    loads are all in flight while this one is multiplied.  Rows that no tile asks for (they fill up 16) hold some row of
+//    the matrix: what they give is not stored.
+//  * A tile reads 1 KB of each operand from LDS per step, two tiles ahead, and its sums stay in a wavefront's registers for
+//    the whole range.
+//  * The last step of a row may be short; it is staged token by token, zeros behind the last one.
 //  * Ranges of tokens are summed by a second kernel, in order; with one range the sums go straight to their places.
 // CKPT: X is a checkpoint (8 bits and an exponent per 32 tokens), widened to T's type on its way into LDS, which is exact
 // but for fp16 values below its normal range.
-template <typename T, bool CKPT, int TILES>
+template <typename T, bool CKPT, int TILES, int PG, int PX>
 __global__ __launch_bounds__(kThreads, 2) void weight_grad_kernel(GradArgs a) {
     constexpr int E = 16 / (int)sizeof(T);       // tokens of a 16-byte piece
     constexpr int STEP = 4 * E;                  // tokens of a step
+    constexpr int XL = CKPT ? STEP / 16 : 4;     // lanes that load a row of X
+    constexpr int GR = kThreads / 4, XR = kThreads / XL; // rows at once
+    constexpr int QX = (PX * 128 + XR - 1) / XR; // loads of X per lane
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
@@ -55,7 +61,7 @@ __global__ __launch_bounds__(kThreads, 2) void weight_grad_kernel(GradArgs a) {
     if (pair >= (pairs * (xcd + 1) >> 3)) return;
     const int split = (int)(pair / a.n_regions);
     const int32_t *reg = a.regions + 8 * (pair % a.n_regions);
-    const int first = reg[0], tiles = reg[1], g_slots = reg[3], slots = reg[4];
+    const int first = reg[0], tiles = reg[1], g_slots = reg[3], x_slots = reg[4] - reg[3];
     const int32_t *rows = a.rows + reg[2];
 
     const int per = (tiles + kGradWaves - 1) / kGradWaves;
@@ -71,83 +77,142 @@ __global__ __launch_bounds__(kThreads, 2) void weight_grad_kernel(GradArgs a) {
 #pragma unroll
     for (int t = 0; t < TILES; ++t) acc[t] = float4v{0.f, 0.f, 0.f, 0.f};
 
-    const int all_steps = (a.N + STEP - 1) / STEP;
+    const int all_steps = (a.N + STEP - 1) / STEP, full = a.N / STEP;
     const int s0 = split * a.per_split, s1 = min(s0 + a.per_split, all_steps);
-    const int q = threadIdx.x & 3;               // this thread's piece of its rows
-    constexpr int kRowsAtOnce = kThreads / 4;
-    constexpr int MAXP = (kGradMaxSlots + kRowsAtOnce - 1) / kRowsAtOnce;
     const uint32_t buffer = (uint32_t)a.slots * kRowBytes;
 
-    uint4v held[MAXP];
+    // this lane's rows: slot i of a pass is row list entry i GR + thread / 4 (the last one again behind the end)
+    const char *gp[PG], *xp[QX];
+    const uint8_t *sp[QX];
+    uint32_t gu[PG], xu[QX];
+    const int gq = threadIdx.x & 3, xq = threadIdx.x % XL;
+#pragma unroll
+    for (int i = 0; i < PG; ++i) {
+        const int slot = min(i * GR + (int)threadIdx.x / 4, g_slots - 1);
+        gp[i] = static_cast<const char *>(a.G) + ((int64_t)rows[slot] * a.ldg + (int64_t)s0 * STEP + gq * E) * (int)sizeof(T);
+        gu[i] = 16u * unit_of((uint32_t)slot, (uint32_t)gq);
+    }
+#pragma unroll
+    for (int i = 0; i < QX; ++i) {
+        const int slot = g_slots + min(i * XR + (int)threadIdx.x / XL, x_slots - 1);
+        const int64_t row = rows[slot];
+        if constexpr (CKPT) {
+            xp[i] = static_cast<const char *>(a.X) + row * a.ldx + (int64_t)s0 * STEP + xq * 16;
+            sp[i] = a.S + row * a.lds + ((int64_t)s0 * STEP >> 5);
+            xu[i] = (uint32_t)slot;
+        } else {
+            xp[i] = static_cast<const char *>(a.X) + (row * a.ldx + (int64_t)s0 * STEP + xq * E) * (int)sizeof(T);
+            xu[i] = 16u * unit_of((uint32_t)slot, (uint32_t)xq);
+        }
+    }
+    uint4v hg[PG], hx[QX];
+    uint32_t hs[QX];
     auto fetch = [&](int s) {
-        const int n0 = s * STEP + q * E;         // first token of the piece
 #pragma unroll
-        for (int i = 0; i < MAXP; ++i) {
-            const int slot = i * kRowsAtOnce + (int)(threadIdx.x >> 2);
-            if (i * kRowsAtOnce >= slots) break;
-            held[i] = uint4v{0u, 0u, 0u, 0u};
-            if (slot >= slots) continue;
-            const int row = rows[slot];
-            if (row < 0 || n0 >= a.N) continue;
-            if (CKPT && slot >= g_slots) {
-                const uint8_t *src = static_cast<const uint8_t *>(a.X) + (int64_t)row * a.ldx + n0;
-                uint32_t b[2] = {0u, 0u};
-                if (n0 + E <= a.N) {
-                    __builtin_memcpy(b, src, E);
-                } else {
+        for (int i = 0; i < PG; ++i) {
+            __builtin_memcpy(&hg[i], gp[i], 16);
+            gp[i] += kRowBytes;
+        }
 #pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (n0 + e < a.N) b[e / 4] |= (uint32_t)src[e] << (8 * (e & 3));
-                }
-                const float scale = exponent_value(a.S[(int64_t)row * a.lds + (n0 >> 5)]);
-                float v[E];
-                e4m3_values<E>(b, scale, v);
-                T w[E];
+        for (int i = 0; i < QX; ++i) {
+            __builtin_memcpy(&hx[i], xp[i], 16);
+            xp[i] += CKPT ? STEP : kRowBytes;
+            if constexpr (CKPT) hs[i] = sp[i][((int64_t)s * STEP >> 5) - ((int64_t)s0 * STEP >> 5)];
+        }
+    };
+    auto put_codes = [&](uint32_t at, uint32_t slot, int q16, const uint32_t (&codes)[4], uint32_t byte) {
+        // 16 values: 16 / E pieces
+        float v[16];
+        e4m3_values<16>(codes, exponent_value(byte), v);
 #pragma unroll
-                for (int e = 0; e < E; ++e) w[e] = from_f32<T>(v[e]);
-                __builtin_memcpy(&held[i], w, 16);
-            } else {
-                const T *src = slot < g_slots ? static_cast<const T *>(a.G) + (int64_t)row * a.ldg + n0
-                                              : static_cast<const T *>(a.X) + (int64_t)row * a.ldx + n0;
-                if (n0 + E <= a.N) {
-                    __builtin_memcpy(&held[i], src, 16);
-                } else {
-                    T w[E];
+        for (int h = 0; h < 16 / E; ++h) {
+            T w[E];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        w[e] = (T)0.f;
-                        if (n0 + e < a.N) w[e] = src[e];
-                    }
-                    __builtin_memcpy(&held[i], w, 16);
-                }
-            }
+            for (int e = 0; e < E; ++e) w[e] = from_f32<T>(v[h * E + e]);
+            uint4v o;
+            __builtin_memcpy(&o, w, 16);
+            *reinterpret_cast<uint4v *>(smem + at + 16u * unit_of(slot, (uint32_t)(q16 * (16 / E) + h))) = o;
         }
     };
     auto put = [&](uint32_t at) {
 #pragma unroll
-        for (int i = 0; i < MAXP; ++i) {
-            const int slot = i * kRowsAtOnce + (int)(threadIdx.x >> 2);
-            if (i * kRowsAtOnce >= slots) break;
-            if (slot < slots) *reinterpret_cast<uint4v *>(smem + at + 16u * unit_of((uint32_t)slot, (uint32_t)q)) = held[i];
+        for (int i = 0; i < PG; ++i) *reinterpret_cast<uint4v *>(smem + at + gu[i]) = hg[i];
+#pragma unroll
+        for (int i = 0; i < QX; ++i) {
+            if constexpr (CKPT) {
+                const uint32_t codes[4] = {hx[i][0], hx[i][1], hx[i][2], hx[i][3]};
+                put_codes(at, xu[i], xq, codes, hs[i]);
+            } else {
+                *reinterpret_cast<uint4v *>(smem + at + xu[i]) = hx[i];
+            }
         }
+    };
+    // the step behind the last full one
+    auto put_short = [&](uint32_t at) {
+        const int n0 = full * STEP;
+        for (int p = threadIdx.x; p < (g_slots + (CKPT ? 0 : x_slots)) * 4; p += kThreads) {
+            const int slot = p >> 2, q = p & 3;
+            const T *src = slot < g_slots ? static_cast<const T *>(a.G) + (int64_t)rows[slot] * a.ldg
+                                          : static_cast<const T *>(a.X) + (int64_t)rows[slot] * a.ldx;
+            T w[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                w[e] = (T)0.f;
+                if (n0 + q * E + e < a.N) w[e] = src[n0 + q * E + e];
+            }
+            uint4v o;
+            __builtin_memcpy(&o, w, 16);
+            *reinterpret_cast<uint4v *>(smem + at + 16u * unit_of((uint32_t)slot, (uint32_t)q)) = o;
+        }
+        if constexpr (CKPT)
+            for (int p = threadIdx.x; p < x_slots * XL; p += kThreads) {
+                const int slot = g_slots + p / XL, q = p % XL;
+                const int64_t row = rows[slot];
+                const uint8_t *src = static_cast<const uint8_t *>(a.X) + row * a.ldx;
+                uint32_t codes[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (n0 + q * 16 + e < a.N) codes[e / 4] |= (uint32_t)src[n0 + q * 16 + e] << (8 * (e & 3));
+                put_codes(at, (uint32_t)slot, q, codes, a.S[row * a.lds + (n0 >> 5)]);
+            }
     };
 
     if (s0 < s1) {
-        fetch(s0);
-        put(0u);
+        if (s0 < full) {
+            fetch(s0);
+            put(0u);
+        } else {
+            put_short(0u);
+        }
     }
     __syncthreads();
     uint32_t at = 0u;
     for (int s = s0; s < s1; ++s) {
-        if (s + 1 < s1) fetch(s + 1);
+        const int next = s + 1;
+        if (next < s1 && next < full) fetch(next);
+        {
+            uint4v x[2][2], y[2][2];
+            auto load = [&](int t) {
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-            const uint4v x = *reinterpret_cast<const uint4v *>(smem + at + 16u * (ops[t] & 0xffffu));
-            const uint4v y = *reinterpret_cast<const uint4v *>(smem + at + 16u * (ops[t] >> 16));
-            acc[t] = product<T>(x, y, acc[t]);
+                for (int h = 0; h < 2; ++h) {
+                    x[(t >> 1) & 1][h] = *reinterpret_cast<const uint4v *>(smem + at + 16u * (ops[t + h] & 0xffffu));
+                    y[(t >> 1) & 1][h] = *reinterpret_cast<const uint4v *>(smem + at + 16u * (ops[t + h] >> 16));
+                }
+            };
+            load(0);
+#pragma unroll
+            for (int t = 0; t < TILES; t += 2) {
+                if (t >= mine) break;
+                if (t + 2 < TILES) load(t + 2);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) acc[t + h] = product<T>(x[(t >> 1) & 1][h], y[(t >> 1) & 1][h], acc[t + h]);
+            }
         }
         at = buffer - at;
-        if (s + 1 < s1) put(at);
+        if (next < s1) {
+            if (next < full) put(at);
+            else put_short(at);
+        }
         __syncthreads();
     }
 
@@ -178,32 +243,36 @@ __global__ __launch_bounds__(256) void weight_sum_kernel(GradArgs a) {
         if ((int32_t)to[e] >= 0) a.out[to[e]] = a.accumulate ? a.out[to[e]] + sum[e] : sum[e];
 }
 
-template <typename T, bool CKPT, int TILES> ubp_status launch_one(const GradArgs &a, hipStream_t st, bool dry) {
+template <typename T, bool CKPT, int SHAPE> ubp_status launch_one(const GradArgs &a, hipStream_t st, bool dry) {
+    constexpr GradShape S = kGradShapes[SHAPE];
+    constexpr auto kernel = &weight_grad_kernel<T, CKPT, S.tiles, S.g_slots / 128, S.x_slots / 128>;
     static LdsLimit limit;
-    const ubp_status rc = limit.raise(reinterpret_cast<const void *>(&weight_grad_kernel<T, CKPT, TILES>));
+    const ubp_status rc = limit.raise(reinterpret_cast<const void *>(kernel));
     if (rc != UBP_OK || dry) return rc;
     const int64_t grid = 8 * (((int64_t)a.n_regions * a.splits + 7) / 8);
     if (grid * kThreads >= (int64_t(1) << 32)) return UBP_ERR_UNSUPPORTED; // (a launch's threads are counted in 32 bits)
-    return launch_kernel(&weight_grad_kernel<T, CKPT, TILES>, dim3((unsigned)grid), dim3(kThreads), (size_t)2 * a.slots * kRowBytes, st, a);
+    return launch_kernel(kernel, dim3((unsigned)grid), dim3(kThreads), (size_t)2 * a.slots * kRowBytes, st, a);
 }
 
-template <typename T, bool CKPT> ubp_status launch_t(const GradArgs &a, int tiles, hipStream_t st, bool dry) {
-    if (tiles <= 2) return launch_one<T, CKPT, 2>(a, st, dry);
-    if (tiles <= 4) return launch_one<T, CKPT, 4>(a, st, dry);
-    if (tiles <= 8) return launch_one<T, CKPT, 8>(a, st, dry);
-    if (tiles <= 16) return launch_one<T, CKPT, 16>(a, st, dry);
-    static_assert(kGradMaxTiles == 28, "the largest instantiation");
-    return launch_one<T, CKPT, kGradMaxTiles>(a, st, dry);
+template <typename T, bool CKPT> ubp_status launch_t(const GradArgs &a, int shape, hipStream_t st, bool dry) {
+    static_assert(kNumGradShapes == 4, "their instantiations");
+    switch (shape) {
+    case 0: return launch_one<T, CKPT, 0>(a, st, dry);
+    case 1: return launch_one<T, CKPT, 1>(a, st, dry);
+    case 2: return launch_one<T, CKPT, 2>(a, st, dry);
+    case 3: return launch_one<T, CKPT, 3>(a, st, dry);
+    }
+    return UBP_ERR_UNSUPPORTED;
 }
 
 } // namespace
 
-ubp_status launch_weight_grad(const GradArgs &a, ubp_dtype dtype, bool checkpoint, int max_tiles, void *stream, bool dry) {
+ubp_status launch_weight_grad(const GradArgs &a, ubp_dtype dtype, bool checkpoint, int shape, void *stream, bool dry) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     switch (dtype) {
-    case UBP_F32: return checkpoint ? launch_t<float, true>(a, max_tiles, st, dry) : launch_t<float, false>(a, max_tiles, st, dry);
-    case UBP_F16: return checkpoint ? launch_t<_Float16, true>(a, max_tiles, st, dry) : launch_t<_Float16, false>(a, max_tiles, st, dry);
-    case UBP_BF16: return checkpoint ? launch_t<__bf16, true>(a, max_tiles, st, dry) : launch_t<__bf16, false>(a, max_tiles, st, dry);
+    case UBP_F32: return checkpoint ? launch_t<float, true>(a, shape, st, dry) : launch_t<float, false>(a, shape, st, dry);
+    case UBP_F16: return checkpoint ? launch_t<_Float16, true>(a, shape, st, dry) : launch_t<_Float16, false>(a, shape, st, dry);
+    case UBP_BF16: return checkpoint ? launch_t<__bf16, true>(a, shape, st, dry) : launch_t<__bf16, false>(a, shape, st, dry);
     }
     return UBP_ERR_INVALID_ARG;
 }

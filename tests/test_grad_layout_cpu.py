@@ -39,7 +39,8 @@ int main(int argc, char **argv) {
     const ubp::GradLayout &L = ubp::get_grad_layout(p);
     CHECK(L.usable && L.built);
     CHECK((int64_t)L.ops.size() == L.n_tiles * 16 && (int64_t)L.inv.size() == L.n_tiles * 256 && (int)L.regions.size() == 8 * L.n_regions);
-    CHECK(L.max_tiles <= ubp::kGradMaxTiles && L.max_slots <= ubp::kGradMaxSlots);
+    const ubp::GradShape S = ubp::kGradShapes[L.shape];
+    CHECK(L.max_tiles <= S.tiles && L.max_g <= S.g_slots && L.max_x <= S.x_slots);
     std::vector<int32_t> start((size_t)nb);
     for (int r = 0; r + bh <= M; ++r)
         for (int32_t b = p->indptr[(size_t)r]; b < p->indptr[(size_t)r + 1]; ++b) start[(size_t)b] = r;
@@ -51,11 +52,11 @@ int main(int argc, char **argv) {
         CHECK(first == next_tile && tiles >= 1 && rows == next_row);
         next_tile += tiles;
         next_row += slots;
-        CHECK(g_slots % 16 == 0 && slots % 16 == 0 && g_slots < slots && slots <= L.max_slots);
+        CHECK(g_slots % 16 == 0 && slots % 16 == 0 && g_slots < slots && slots <= L.max_slots && g_slots <= L.max_g && slots - g_slots <= L.max_x);
         CHECK((tiles + ubp::kGradWaves - 1) / ubp::kGradWaves <= L.max_tiles);
         for (int64_t s = 0; s < slots; ++s) {
             const int32_t row = L.rows[(size_t)(rows + s)];
-            CHECK(row >= -1 && row < (s < g_slots ? M : K));
+            CHECK(row >= 0 && row < (s < g_slots ? M : K));
         }
         for (int64_t t = first; t < first + tiles; ++t) {
             int32_t gr[16], xr[16];
