@@ -590,12 +590,6 @@ ubp_status checkpoint(const ubp_packed *p, bool save, void *X, int64_t ldx, int3
     return save ? launch_save(a, p->dtype, stream) : launch_load(a, p->dtype, stream);
 }
 
-// Tokens of a step of the weight gradient: 64 bytes of a row.
-int64_t grad_steps(const ubp_packed *p, int32_t N) {
-    const int64_t per = 64 / dtype_size(p->dtype);
-    return ((int64_t)N + per - 1) / per;
-}
-
 ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const void *X, int64_t ldx, const uint8_t *S, int64_t lds, bool saved,
                        int32_t N, float *dvalues, int32_t accumulate, void *workspace, int64_t workspace_bytes, void *stream, bool dry) try {
     if (!p || p->device == UBP_HOST_ONLY || N < 0) return UBP_ERR_INVALID_ARG;
@@ -628,7 +622,11 @@ ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const vo
     a.lds = lds;
     a.N = N;
     a.n_regions = L->n_regions;
+    a.M = p->M;
+    a.K = p->K;
     a.slots = L->max_slots;
+    a.slots_g = L->max_g;
+    a.slots_x = L->max_x;
     a.n_tiles = L->n_tiles;
     a.out = dvalues;
     a.accumulate = accumulate ? 1 : 0;
@@ -641,9 +639,10 @@ ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const vo
         if (accumulate) return UBP_OK;
         return launch_weight_sum(a, stream); // (a sum of no ranges)
     }
-    const int64_t steps = grad_steps(p, N);
-    a.splits = grad_splits(*L, steps);
-    a.per_split = (int)((steps + a.splits - 1) / a.splits);
+    const GradRanges ranges = grad_ranges(*L, N);
+    a.splits = ranges.splits;
+    a.per_split = ranges.tokens;
+    a.blocks = ranges.tokens % kGradBlock == 0;
     if (a.splits > 1) {
         if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0 || workspace_bytes < a.splits * L->n_tiles * 1024) return UBP_ERR_INVALID_ARG;
         a.part = static_cast<float *>(workspace);
@@ -721,7 +720,7 @@ int64_t ubp_weight_grad_workspace(const ubp_packed *p, int32_t N) {
         std::lock_guard<std::mutex> hold(p->lock);
         const ubp::GradLayout &L = ubp::get_grad_layout(p);
         if (!L.usable) return -1;
-        const int splits = ubp::grad_splits(L, ubp::grad_steps(p, N));
+        const int splits = ubp::grad_ranges(L, N).splits;
         return splits > 1 ? splits * L.n_tiles * 1024 : 0;
     } catch (...) {
         return -1;

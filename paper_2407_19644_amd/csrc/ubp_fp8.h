@@ -14,21 +14,31 @@ __device__ __forceinline__ uint32_t exponent_byte(uint32_t top) {
     const int b = (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
     return (uint32_t)max(b, 0);
 }
-__device__ __forceinline__ float exponent_value(uint32_t byte) { // 2^(byte - 127)
-    return __builtin_bit_cast(float, byte == 0u ? 0x00400000u : byte << 23);
-}
 __device__ __forceinline__ float exponent_inverse(uint32_t byte) { return __builtin_bit_cast(float, (254u - byte) << 23); }
 
-// E (4 or a multiple of 4) codes -> their values times scale
-template <int E> __device__ __forceinline__ void e4m3_values(const uint32_t *codes, float scale, float (&v)[E]) {
-    typedef float float2v __attribute__((ext_vector_type(2)));
+// E (4 or a multiple of 4) codes -> their values times the power of two of an exponent byte, in T, to nearest.  The
+// conversion takes its power from the exponent bits of a float alone: the byte itself, 0 for 2^-127 included.  (For every code and
+// every byte but 255 its results are those of a product in fp32 and a rounding to T.)
+template <typename T, int E> __device__ __forceinline__ void e4m3_to(const uint32_t *codes, uint32_t byte, T *out) {
+    const float scale = __builtin_bit_cast(float, byte << 23);
 #pragma unroll
     for (int w = 0; w < E / 4; ++w) {
-        const float2v lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[w], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[w], true);
-        v[4 * w] = lo[0] * scale;
-        v[4 * w + 1] = lo[1] * scale;
-        v[4 * w + 2] = hi[0] * scale;
-        v[4 * w + 3] = hi[1] * scale;
+        if constexpr (__is_same(T, __bf16)) {
+            const auto lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[w], scale, false);
+            const auto hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[w], scale, true);
+            __builtin_memcpy(out + 4 * w, &lo, 4);
+            __builtin_memcpy(out + 4 * w + 2, &hi, 4);
+        } else if constexpr (__is_same(T, _Float16)) {
+            const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes[w], scale, false);
+            const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes[w], scale, true);
+            __builtin_memcpy(out + 4 * w, &lo, 4);
+            __builtin_memcpy(out + 4 * w + 2, &hi, 4);
+        } else {
+            const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes[w], scale, false);
+            const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes[w], scale, true);
+            __builtin_memcpy(out + 4 * w, &lo, 8);
+            __builtin_memcpy(out + 4 * w + 2, &hi, 8);
+        }
     }
 }
 

@@ -128,7 +128,7 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
         return Rows{padded(g.size()), padded(x.size())};
     };
     if (n) open.push_back({0, n, slots(order.data(), n)});
-    auto rows_fit = [](const Rows &r) { return r.g <= kGradLargest.g_slots && r.x <= kGradLargest.x_slots; };
+    auto rows_fit = [](const Rows &r) { return r.g <= kGradLargest.g_slots && r.x <= kGradLargest.x_slots && r.all() <= kGradSlots; };
     // (halves that need not be cut again for their rows come first)
     auto cost = [&](const Rows (&h)[2]) {
         return h[0].all() + h[1].all() + (rows_fit(h[0]) ? 0 : int64_t(1) << 40) + (rows_fit(h[1]) ? 0 : int64_t(1) << 40);
@@ -207,12 +207,16 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
     return L;
 }
 
-// Ranges of tokens that the sum is cut into: the regions of all ranges fill the CUs about once, and a range has at least
-// kGradMinSteps steps.
-int grad_splits(const GradLayout &L, int64_t steps) {
-    if (L.n_regions == 0 || steps <= 0) return 1;
-    const int64_t fill = std::max<int64_t>(1, kGradWorkgroups / L.n_regions);
-    return (int)std::max<int64_t>(1, std::min(fill, steps / kGradMinSteps));
+// The regions of all ranges fill the CUs about once.  Ranges are whole blocks of tokens where there are blocks enough for
+// that; of few tokens they are as short as kGradMinTokens.
+GradRanges grad_ranges(const GradLayout &L, int64_t N) {
+    const int64_t fill = L.n_regions ? std::max<int64_t>(1, kGradWorkgroups / L.n_regions) : 1;
+    const int64_t unit = N >= fill * kGradBlock ? kGradBlock : kGradUnit;
+    const int64_t most = std::max<int64_t>(1, std::min(fill, N / kGradMinTokens));
+    const int64_t units = std::max<int64_t>(1, unit == kGradBlock ? N / unit : (N + unit - 1) / unit); // (a short block belongs to the last range)
+    const int64_t each = (units + most - 1) / most;
+    const int64_t splits = (units + each - 1) / each;                       // (none of them empty)
+    return {(int)splits, (int)(each * unit)};
 }
 
 } // namespace ubp

@@ -215,20 +215,22 @@ struct Wros4Layout {
     std::vector<int32_t> rec_of_row, rec_of_end, row_of_rec;
 };
 
-// Weight gradient: wavefronts of a workgroup, regions that a layer is cut into where its tiles allow, workgroups that fill
-// the card, steps of a range of tokens at least.
+// Weight gradient: wavefronts of a workgroup that multiply, regions that a layer is cut into where its tiles allow, workgroups
+// that fill the card, tokens of a range at least and its unit, LDS rows (of at most 64 bytes per stage) of a region and stages
+// of the ring at most.
 constexpr int kGradWaves = 8;
 constexpr int kGradRegions = 32;
 constexpr int kGradWorkgroups = 256;
-constexpr int kGradMinSteps = 4;
-
-// Tiles a wavefront keeps, LDS rows (of 64 bytes, in two buffers) for G and for X of a region, at most, per instantiation of
-// the kernel.
+constexpr int kGradMinTokens = 64;
+constexpr int kGradUnit = 32, kGradBlock = 128;
+constexpr int kGradSlots = 832;
+constexpr int kGradMaxRing = 8;
+// Tiles a wavefront keeps and LDS rows for G and for X of a region, at most, per instantiation of the kernels.
 struct GradShape { int tiles, g_slots, x_slots; };
-constexpr int kNumGradShapes = 4;
-constexpr GradShape kGradShapes[kNumGradShapes] = {{2, 256, 256}, {4, 256, 256}, {8, 384, 384}, {16, 640, 640}};
+constexpr int kNumGradShapes = 3;
+constexpr GradShape kGradShapes[kNumGradShapes] = {{2, 256, 256}, {4, 256, 256}, {8, 640, 640}};
 constexpr GradShape kGradLargest = kGradShapes[kNumGradShapes - 1];
-static_assert((kGradLargest.g_slots + kGradLargest.x_slots) * 128 <= 160 * 1024, "two buffers fit LDS");
+static_assert(kGradSlots * 64 * 3 <= 160 * 1024 && kGradSlots * 64 <= 65536, "three stages fit LDS; places in a stage have 16 bits");
 
 // Host image of the weight gradient's layout.  A tile is the product of 16 consecutive rows of G with 16 rows of X; a region
 // is a run of tiles that one workgroup keeps in registers, with the rows of G and X that they need.
@@ -398,9 +400,11 @@ struct GradArgs {
     const void *G, *X;        // X: rows of the layer's type, or of a checkpoint's bytes
     const uint8_t *S;         // the checkpoint's exponents
     int64_t ldg, ldx, lds;
-    int N, n_regions, splits;
-    int per_split;            // steps of a range
-    int slots;                // LDS rows of a buffer
+    int M, K, N, n_regions, splits;
+    int per_split;            // tokens of a range (in the kernels: steps)
+    int blocks;               // ranges are whole blocks of kGradBlock tokens but for the last one's end
+    int slots, slots_g, slots_x; // LDS rows of a region, of G and of X, at most
+    int stage_bytes, ring;    // of the ring of stages
     int64_t n_tiles;
     float *out;               // dvalues
     float *part;              // [splits][tiles][256], where splits > 1
@@ -503,7 +507,9 @@ const TileLayout &get_tile_layout(const ubp_packed *p);
 const DirectLayout &get_direct_layout(const ubp_packed *p);
 const Wros4Layout &get_wros4_layout(const ubp_packed *p);
 const GradLayout &get_grad_layout(const ubp_packed *p);
-int grad_splits(const GradLayout &L, int64_t steps);
+// Ranges that the sum over N tokens is cut into, and the tokens of each (the last one takes what is left).
+struct GradRanges { int splits, tokens; };
+GradRanges grad_ranges(const GradLayout &L, int64_t N);
 const MaskStats &get_mask_stats(const ubp_packed *p);
 // Stripes per wavefront of the gather kernel.  They follow the block height: a 16-row block touches two stripes
 // anyway, so tall row groups cost little extra zero fill and divide the staging of X by the rows a workgroup

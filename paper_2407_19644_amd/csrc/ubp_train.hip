@@ -203,15 +203,8 @@ __global__ __launch_bounds__(256) void load_kernel(CheckpointArgs a) {
         for (int e = 0; e < kLaneValues; ++e)
             if (col + e < a.N) q[e / 4] |= (uint32_t)src[e] << (8 * (e & 3));
     }
-    float v[kLaneValues];
-    e4m3_values<kLaneValues>(q, exponent_value(a.S[row * a.lds + col / kGroup]), v);
     T o[kLaneValues];
-#pragma unroll
-    for (int e = 0; e < kLaneValues; ++e) {
-        // (the product and its rounding to fp16 as one instruction, which adds +0, would lose the sign of -0)
-        if constexpr (__is_same(T, _Float16)) asm("" : "+v"(v[e]));
-        o[e] = from_f32<T>(v[e]);
-    }
+    e4m3_to<T, kLaneValues>(q, a.S[row * a.lds + col / kGroup], o);
     T *dst = static_cast<T *>(a.out) + row * a.ldx + col;
     if (col + kLaneValues <= a.N) {
         __builtin_memcpy(dst, o, sizeof o);

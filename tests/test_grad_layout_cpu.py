@@ -40,7 +40,7 @@ int main(int argc, char **argv) {
     CHECK(L.usable && L.built);
     CHECK((int64_t)L.ops.size() == L.n_tiles * 16 && (int64_t)L.inv.size() == L.n_tiles * 256 && (int)L.regions.size() == 8 * L.n_regions);
     const ubp::GradShape S = ubp::kGradShapes[L.shape];
-    CHECK(L.max_tiles <= S.tiles && L.max_g <= S.g_slots && L.max_x <= S.x_slots);
+    CHECK(L.max_tiles <= S.tiles && L.max_g <= S.g_slots && L.max_x <= S.x_slots && L.max_slots <= ubp::kGradSlots);
     std::vector<int32_t> start((size_t)nb);
     for (int r = 0; r + bh <= M; ++r)
         for (int32_t b = p->indptr[(size_t)r]; b < p->indptr[(size_t)r + 1]; ++b) start[(size_t)b] = r;
@@ -82,9 +82,11 @@ int main(int argc, char **argv) {
     }
     CHECK(next_tile == L.n_tiles && next_row == (int64_t)L.rows.size());
     for (char c : seen) CHECK(c);
-    for (int64_t steps : {0, 1, 3, 4, 7, 8, 31, 256, 392, 4096, 1 << 26}) {
-        const int64_t s = ubp::grad_splits(L, steps);
-        CHECK(s >= 1 && s <= 256 && (s == 1 || s * ubp::kGradMinSteps <= steps));
+    for (int64_t n : {0, 1, 63, 64, 65, 127, 128, 129, 1567, 4096, 8192, 12543, 1 << 20, 0x7fffffff}) {
+        const ubp::GradRanges r = ubp::grad_ranges(L, n);
+        CHECK(r.splits >= 1 && r.splits <= 256 && r.tokens >= 32 && r.tokens % 32 == 0);
+        CHECK(r.splits == 1 || (int64_t)(r.splits - 1) * r.tokens < n);
+        CHECK((int64_t)r.splits * r.tokens + 127 >= n);
     }
     std::printf("%lld tiles %d regions %d of a wavefront %d rows\n", (long long)L.n_tiles, L.n_regions, L.max_tiles, L.max_slots);
     ubp_packed_free(p);
@@ -131,7 +133,7 @@ def test_refusals_without_a_device():
     from layer_util import layer
     blocks, W, _ = layer(64, 48, 4, 4, 0.3, "f16", 1)
     p = ubp.pack(W, "f16", 4, 4, blocks)
-    assert ubp.weight_grad_workspace(p, 0) == 0 and ubp.weight_grad_workspace(p, 1) == 0
+    assert ubp.weight_grad_workspace(p, 0) == 0 and ubp.weight_grad_workspace(p, 127) == 0
     assert ubp.weight_grad_workspace(p, 100000) > 0 and ubp.weight_grad_workspace(p, 100000) % 1024 == 0
     assert ubp.linear_grad_workspace(p, 8192) == 0 and ubp.linear_grad_workspace(p, 8193) == 64 * 2 * 4
     for call in (lambda: ubp.weight_grad_workspace(p, -1), lambda: ubp.linear_grad_workspace(p, -1)):

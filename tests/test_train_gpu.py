@@ -260,6 +260,9 @@ GRAD_CASES = [  # M, K, N, bh, bw, density, dtype
     (256, 600, 4096, 4, 4, 0.25, "bf16"), (130, 600, 1001, 16, 16, 0.15, "bf16"), (40, 50, 17, 40, 50, 1.0, "bf16"),
     (16, 16, 32, 16, 16, 1.0, "bf16"), (1, 1, 5, 1, 1, 1.0, "bf16"), (512, 512, 64, 4, 1, 0.2, "bf16"), (700, 800, 300, 2, 3, 0.3, "bf16"),
     (2048, 1024, 520, 16, 16, 0.15, "bf16"), (1500, 1400, 40, 16, 16, 0.2, "f32"),
+    # many tokens in rows of 16-byte pieces, with and without tokens behind the last block of 128
+    (256, 300, 4096, 16, 16, 0.2, "bf16"), (130, 200, 2064, 8, 8, 0.25, "f16"), (90, 500, 1040, 4, 4, 0.3, "f32"), (96, 2304, 6288, 4, 4, 0.25, "bf16"),
+    (1100, 1000, 1424, 16, 16, 0.25, "bf16"), (24, 16, 34000, 4, 4, 0.5, "f16"), (700, 640, 2176, 16, 16, 0.3, "f32"),
 ]
 
 
@@ -276,21 +279,24 @@ def test_weight_grad(case):
     tol = weight_tolerance(G64, X64, rows, cols, N)
     got = run_weight_grad(p, G, X, dtype, rows.size)
     assert (np.abs(got - want) <= tol).all(), float((np.abs(got - want) / tol).max())
-    # other pitches and alignments: the same sums in the same order
-    for ldg, ldx, off in ((N + 1, N + 3, 1), (N + 8, N + 16, 8), (N + 5, N, 3)):
-        assert np.array_equal(run_weight_grad(p, G, X, dtype, rows.size, ldg=ldg, ldx=ldx, off=off), got)
+    # other pitches and alignments (the general kernel, or the one for rows of 16-byte pieces)
+    for ldg, ldx, off in ((N + 1, N + 3, 1), (N + 8, N + 16, 8), (N + 5, N, 3), (-(-N // 16) * 16, -(-N // 16) * 16 + 16, 0)):
+        other = run_weight_grad(p, G, X, dtype, rows.size, ldg=ldg, ldx=ldx, off=off)
+        assert (np.abs(other - want) <= tol).all(), (ldg, ldx, off)
+        assert np.array_equal(other, run_weight_grad(p, G, X, dtype, rows.size, ldg=ldg, ldx=ldx, off=off))
     # added to what is there
     init = np.linspace(-3, 3, rows.size).astype(np.float32)
     acc = run_weight_grad(p, G, X, dtype, rows.size, accumulate=True, init=init, repeat=2)
     assert (np.abs(acc - (init + 2 * want)) <= 2 * tol + 2.0 ** -22 * (np.abs(init) + 2 * np.abs(want))).all()
-    # from a checkpoint: what the loaded values give, bit for bit
+    # from a checkpoint: what the loaded values give (bit for bit where both run the same kernel)
     codes, exps, vals = checkpoint_of(X64, dtype)
     X8 = encode(vals.astype(np.float32), dtype)
-    got8 = run_weight_grad(p, G, None, dtype, rows.size, ckpt=(codes, exps))
-    assert np.array_equal(got8, run_weight_grad(p, G, X8, dtype, rows.size))
-    assert np.array_equal(got8, run_weight_grad(p, G, None, dtype, rows.size, ckpt=(codes, exps), ldg=N + 3, ldx=N + 5, off=7))
     want8 = (G64 @ decode_f64(X8, dtype).T)[rows, cols]
-    assert (np.abs(got8 - want8) <= tol * 2).all()
+    for ldg, ldx, off in ((N, N, 0), (N + 3, N + 5, 7), (-(-N // 16) * 16, -(-N // 16) * 16 + 16, 0)):
+        got8 = run_weight_grad(p, G, None, dtype, rows.size, ckpt=(codes, exps), ldg=ldg, ldx=ldx, off=off)
+        assert (np.abs(got8 - want8) <= tol * 2).all(), (ldg, ldx, off)
+        if (ldg, off) != (N, 0):
+            assert np.array_equal(got8, run_weight_grad(p, G, X8, dtype, rows.size, ldg=ldg, ldx=ldx, off=off))
     p.free()
 
 
