@@ -622,9 +622,6 @@ ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const vo
     a.lds = lds;
     a.N = N;
     a.n_regions = L->n_regions;
-    a.M = p->M;
-    a.K = p->K;
-    a.slots = L->max_slots;
     a.slots_g = L->max_g;
     a.slots_x = L->max_x;
     a.n_tiles = L->n_tiles;
@@ -642,7 +639,6 @@ ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const vo
     const GradRanges ranges = grad_ranges(*L, N);
     a.splits = ranges.splits;
     a.per_split = ranges.tokens;
-    a.blocks = ranges.tokens % kGradBlock == 0;
     if (a.splits > 1) {
         if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0 || workspace_bytes < a.splits * L->n_tiles * 1024) return UBP_ERR_INVALID_ARG;
         a.part = static_cast<float *>(workspace);

@@ -207,16 +207,13 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
     return L;
 }
 
-// The regions of all ranges fill the CUs about once.  Ranges are whole blocks of tokens where there are blocks enough for
-// that; of few tokens they are as short as kGradMinTokens.
+// The regions of all ranges fill the CUs about once, and a range has kGradMinTokens tokens at least.
 GradRanges grad_ranges(const GradLayout &L, int64_t N) {
     const int64_t fill = L.n_regions ? std::max<int64_t>(1, kGradWorkgroups / L.n_regions) : 1;
-    const int64_t unit = N >= fill * kGradBlock ? kGradBlock : kGradUnit;
+    const int64_t units = std::max<int64_t>(1, N / kGradUnit);             // (a short unit belongs to the last range)
     const int64_t most = std::max<int64_t>(1, std::min(fill, N / kGradMinTokens));
-    const int64_t units = std::max<int64_t>(1, unit == kGradBlock ? N / unit : (N + unit - 1) / unit); // (a short block belongs to the last range)
     const int64_t each = (units + most - 1) / most;
-    const int64_t splits = (units + each - 1) / each;                       // (none of them empty)
-    return {(int)splits, (int)(each * unit)};
+    return {(int)((units + each - 1) / each), (int)(each * kGradUnit)};    // (none of them empty)
 }
 
 } // namespace ubp

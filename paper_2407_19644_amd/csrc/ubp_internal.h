@@ -215,22 +215,20 @@ struct Wros4Layout {
     std::vector<int32_t> rec_of_row, rec_of_end, row_of_rec;
 };
 
-// Weight gradient: wavefronts of a workgroup that multiply, regions that a layer is cut into where its tiles allow, workgroups
-// that fill the card, tokens of a range at least and its unit, LDS rows (of at most 64 bytes per stage) of a region and stages
-// of the ring at most.
-constexpr int kGradWaves = 8;
+// Weight gradient: wavefronts of a workgroup, regions that a layer is cut into where its tiles allow, workgroups that fill
+// the card, tokens of a range at least and its unit, LDS rows (of at most 128 bytes) of a region at most.
+constexpr int kGradWaves = 16;
 constexpr int kGradRegions = 32;
 constexpr int kGradWorkgroups = 256;
-constexpr int kGradMinTokens = 64;
-constexpr int kGradUnit = 32, kGradBlock = 128;
-constexpr int kGradSlots = 832;
-constexpr int kGradMaxRing = 8;
-// Tiles a wavefront keeps and LDS rows for G and for X of a region, at most, per instantiation of the kernels.
+constexpr int kGradUnit = 64;
+constexpr int kGradMinTokens = 2 * kGradUnit;
+constexpr int kGradSlots = 1264;
+// Tiles a wavefront keeps and LDS rows for G and for X of a region, at most, per instantiation of the kernel.
 struct GradShape { int tiles, g_slots, x_slots; };
 constexpr int kNumGradShapes = 3;
-constexpr GradShape kGradShapes[kNumGradShapes] = {{2, 256, 256}, {4, 256, 256}, {8, 640, 640}};
+constexpr GradShape kGradShapes[kNumGradShapes] = {{2, 256, 256}, {4, 384, 384}, {8, 640, 640}};
 constexpr GradShape kGradLargest = kGradShapes[kNumGradShapes - 1];
-static_assert(kGradSlots * 64 * 3 <= 160 * 1024 && kGradSlots * 64 <= 65536, "three stages fit LDS; places in a stage have 16 bits");
+static_assert(kGradSlots * 128 <= 160 * 1024, "a stage fits LDS");
 
 // Host image of the weight gradient's layout.  A tile is the product of 16 consecutive rows of G with 16 rows of X; a region
 // is a run of tiles that one workgroup keeps in registers, with the rows of G and X that they need.
@@ -400,11 +398,9 @@ struct GradArgs {
     const void *G, *X;        // X: rows of the layer's type, or of a checkpoint's bytes
     const uint8_t *S;         // the checkpoint's exponents
     int64_t ldg, ldx, lds;
-    int M, K, N, n_regions, splits;
-    int per_split;            // tokens of a range (in the kernels: steps)
-    int blocks;               // ranges are whole blocks of kGradBlock tokens but for the last one's end
-    int slots, slots_g, slots_x; // LDS rows of a region, of G and of X, at most
-    int stage_bytes, ring;    // of the ring of stages
+    int N, n_regions, splits;
+    int per_split;            // tokens of a range (in the kernel: stages); the last one takes what is left
+    int slots_g, slots_x;     // LDS rows of a region, of G and of X, at most
     int64_t n_tiles;
     float *out;               // dvalues
     float *part;              // [splits][tiles][256], where splits > 1

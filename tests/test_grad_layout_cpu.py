@@ -84,9 +84,9 @@ int main(int argc, char **argv) {
     for (char c : seen) CHECK(c);
     for (int64_t n : {0, 1, 63, 64, 65, 127, 128, 129, 1567, 4096, 8192, 12543, 1 << 20, 0x7fffffff}) {
         const ubp::GradRanges r = ubp::grad_ranges(L, n);
-        CHECK(r.splits >= 1 && r.splits <= 256 && r.tokens >= 32 && r.tokens % 32 == 0);
+        CHECK(r.splits >= 1 && r.splits <= 256 && r.tokens >= 64 && r.tokens % 64 == 0);
         CHECK(r.splits == 1 || (int64_t)(r.splits - 1) * r.tokens < n);
-        CHECK((int64_t)r.splits * r.tokens + 127 >= n);
+        CHECK((int64_t)r.splits * r.tokens + 63 >= n);
     }
     std::printf("%lld tiles %d regions %d of a wavefront %d rows\n", (long long)L.n_tiles, L.n_regions, L.max_tiles, L.max_slots);
     ubp_packed_free(p);
@@ -133,7 +133,7 @@ def test_refusals_without_a_device():
     from layer_util import layer
     blocks, W, _ = layer(64, 48, 4, 4, 0.3, "f16", 1)
     p = ubp.pack(W, "f16", 4, 4, blocks)
-    assert ubp.weight_grad_workspace(p, 0) == 0 and ubp.weight_grad_workspace(p, 127) == 0
+    assert ubp.weight_grad_workspace(p, 0) == 0 and ubp.weight_grad_workspace(p, 255) == 0
     assert ubp.weight_grad_workspace(p, 100000) > 0 and ubp.weight_grad_workspace(p, 100000) % 1024 == 0
     assert ubp.linear_grad_workspace(p, 8192) == 0 and ubp.linear_grad_workspace(p, 8193) == 64 * 2 * 4
     for call in (lambda: ubp.weight_grad_workspace(p, -1), lambda: ubp.linear_grad_workspace(p, -1)):
