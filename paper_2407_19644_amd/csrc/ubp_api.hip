@@ -622,8 +622,6 @@ ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const vo
     a.lds = lds;
     a.N = N;
     a.n_regions = L->n_regions;
-    a.slots_g = L->max_g;
-    a.slots_x = L->max_x;
     a.n_tiles = L->n_tiles;
     a.out = dvalues;
     a.accumulate = accumulate ? 1 : 0;

@@ -16,11 +16,10 @@ __device__ __forceinline__ uint32_t exponent_byte(uint32_t top) {
 }
 __device__ __forceinline__ float exponent_inverse(uint32_t byte) { return __builtin_bit_cast(float, (254u - byte) << 23); }
 
-// E (4 or a multiple of 4) codes -> their values times the power of two of an exponent byte, in T, to nearest.  The
-// conversion takes its power from the exponent bits of a float alone: the byte itself, 0 for 2^-127 included.  (For every code and
-// every byte but 255 its results are those of a product in fp32 and a rounding to T.)
-template <typename T, int E> __device__ __forceinline__ void e4m3_to(const uint32_t *codes, uint32_t byte, T *out) {
-    const float scale = __builtin_bit_cast(float, byte << 23);
+// E (4 or a multiple of 4) codes -> their values times a power of two, in T, to nearest.  The conversion takes the power from
+// the exponent bits of `scale` alone, the exponent byte itself, 0 for 2^-127 included.  (For every code and every byte but
+// 255 its results are those of a product in fp32 and a rounding to T.)
+template <typename T, int E> __device__ __forceinline__ void e4m3_to(const uint32_t *codes, float scale, T *out) {
 #pragma unroll
     for (int w = 0; w < E / 4; ++w) {
         if constexpr (__is_same(T, __bf16)) {

@@ -128,7 +128,7 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
         return Rows{padded(g.size()), padded(x.size())};
     };
     if (n) open.push_back({0, n, slots(order.data(), n)});
-    auto rows_fit = [](const Rows &r) { return r.g <= kGradLargest.g_slots && r.x <= kGradLargest.x_slots && r.all() <= kGradSlots; };
+    auto rows_fit = [](const Rows &r) { return r.g <= kGradLargest.g_slots && r.x <= kGradLargest.x_slots; };
     // (halves that need not be cut again for their rows come first)
     auto cost = [&](const Rows (&h)[2]) {
         return h[0].all() + h[1].all() + (rows_fit(h[0]) ? 0 : int64_t(1) << 40) + (rows_fit(h[1]) ? 0 : int64_t(1) << 40);

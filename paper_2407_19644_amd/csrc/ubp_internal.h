@@ -216,19 +216,17 @@ struct Wros4Layout {
 };
 
 // Weight gradient: wavefronts of a workgroup, regions that a layer is cut into where its tiles allow, workgroups that fill
-// the card, tokens of a range at least and its unit, LDS rows (of at most 128 bytes) of a region at most.
+// the card, tokens of a range at least and its unit.
 constexpr int kGradWaves = 16;
 constexpr int kGradRegions = 32;
 constexpr int kGradWorkgroups = 256;
 constexpr int kGradUnit = 64;
 constexpr int kGradMinTokens = 2 * kGradUnit;
-constexpr int kGradSlots = 1264;
 // Tiles a wavefront keeps and LDS rows for G and for X of a region, at most, per instantiation of the kernel.
 struct GradShape { int tiles, g_slots, x_slots; };
 constexpr int kNumGradShapes = 3;
 constexpr GradShape kGradShapes[kNumGradShapes] = {{2, 256, 256}, {4, 384, 384}, {8, 640, 640}};
 constexpr GradShape kGradLargest = kGradShapes[kNumGradShapes - 1];
-static_assert(kGradSlots * 128 <= 160 * 1024, "a stage fits LDS");
 
 // Host image of the weight gradient's layout.  A tile is the product of 16 consecutive rows of G with 16 rows of X; a region
 // is a run of tiles that one workgroup keeps in registers, with the rows of G and X that they need.
@@ -400,7 +398,6 @@ struct GradArgs {
     int64_t ldg, ldx, lds;
     int N, n_regions, splits;
     int per_split;            // tokens of a range (in the kernel: stages); the last one takes what is left
-    int slots_g, slots_x;     // LDS rows of a region, of G and of X, at most
     int64_t n_tiles;
     float *out;               // dvalues
     float *part;              // [splits][tiles][256], where splits > 1

@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256) void load_kernel(CheckpointArgs a) {
             if (col + e < a.N) q[e / 4] |= (uint32_t)src[e] << (8 * (e & 3));
     }
     T o[kLaneValues];
-    e4m3_to<T, kLaneValues>(q, a.S[row * a.lds + col / kGroup], o);
+    e4m3_to<T, kLaneValues>(q, __builtin_bit_cast(float, (uint32_t)a.S[row * a.lds + col / kGroup] << 23), o);
     T *dst = static_cast<T *>(a.out) + row * a.ldx + col;
     if (col + kLaneValues <= a.N) {
         __builtin_memcpy(dst, o, sizeof o);

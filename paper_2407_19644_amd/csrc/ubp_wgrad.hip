@@ -11,12 +11,11 @@ namespace {
 constexpr int kRowBytes = 128; // of a row of G or X that a stage takes: 64 16-bit or 32 fp32 tokens, a cache line
 constexpr int kThreads = 64 * kGradWaves;
 
-// Place of 16-byte piece q of LDS row r: 16 neighbouring rows of one piece lie in all 16 units of 256 bytes, i.e. in all 64
-// banks, for rows of 128, 64 (a checkpoint's 64 codes) and 32 bytes (32 codes).
+// A stage lies in LDS in two halves, each with rows of BYTES bytes: 64 of G and X, 32 or 16 of a checkpoint's codes.  Place of
+// 16-byte piece q of row r of a half: 16 neighbouring rows of one piece lie in all 16 units of 256 bytes, i.e. in all 64 banks.
 template <int BYTES> __device__ __forceinline__ uint32_t place(uint32_t r, uint32_t q) {
-    static_assert(BYTES == 128 || BYTES == 64 || BYTES == 32, "a row of a stage");
-    constexpr int shift = BYTES == 128 ? 1 : BYTES == 64 ? 2 : 3;
-    return r * BYTES + 16u * (q ^ ((r >> shift) & (BYTES / 16 - 1)));
+    static_assert(BYTES == 64 || BYTES == 32 || BYTES == 16, "a row of half a stage");
+    return r * BYTES + 16u * (BYTES == 64 ? q ^ ((r >> 2) & 3u) : BYTES == 32 ? q ^ ((r >> 3) & 1u) : q);
 }
 
 template <typename T> __device__ __forceinline__ float4v product(uint4v a, uint4v b, float4v c);
@@ -32,6 +31,26 @@ template <> __device__ __forceinline__ float4v product<float>(uint4v a, uint4v b
 #pragma unroll
     for (int m = 0; m < 4; ++m) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[m], y[m], c, 0, 0, 0);
     return c;
+}
+
+// The first `count` of the elements that 16 bytes hold, zeros behind them; nothing behind them is read.  (Where not all are
+// there, one by one, the last first: loads of all at once would take registers that the whole kernel then lacks.)
+template <typename T> __device__ __forceinline__ uint4v first_of(const T *src, int count) {
+    constexpr int E = 16 / (int)sizeof(T), BITS = 8 * (int)sizeof(T);
+    uint4v o = {0u, 0u, 0u, 0u};
+    if (count >= E) {
+        __builtin_memcpy(&o, src, 16);
+        return o;
+    }
+#pragma unroll 1
+    for (int k = count - 1; k >= 0; --k) {
+        uint32_t v = 0u;
+        __builtin_memcpy(&v, src + k, sizeof(T));
+#pragma unroll
+        for (int w = 3; w >= 0; --w) o[w] = (BITS < 32 ? o[w] << (BITS & 31) : 0u) | (w > 0 ? o[w > 0 ? w - 1 : 0] >> ((32 - BITS) & 31) : 0u);
+        o[0] |= v;
+    }
+    return o;
 }
 
 // A tile's sums: of one range of several, or, where there is only one, at their places.
@@ -52,8 +71,9 @@ __device__ __forceinline__ void store_tile(const GradArgs &a, float4v sum, int s
 //  * A stage = 128 bytes (a cache line, where rows begin at one) of every row that the region needs, 64 of a checkpoint's,
 //    through registers into LDS, which holds one stage: a row's register is loaded again as soon as it has been written
 //    there, so that loads are in flight all the time.  Rows of any alignment and pitch.
-//  * A tile reads 1 KB of each operand from LDS per half a stage, a tile ahead, and its sums stay in a wavefront's
-//    registers for the whole range.
+//  * A tile reads 1 KB of each operand from LDS per half a stage (both halves at addresses a constant apart; the rows of G
+//    once for tiles of one window), and its sums stay in a wavefront's registers for the whole range.  The other wavefronts
+//    of the SIMD, three of them, cover the way from LDS: operands fetched a tile ahead took registers, and no less time.
 //  * CKPT: X is a checkpoint.  Its codes stay as they are in LDS, and a lane widens its 8 codes of a tile by 4 conversions that
 //    take the exponent along: exact but for fp16 values below its normal range.  Exponents come 16 at a time.
 //  * The last stage of a row may be short; it is staged token by token, zeros behind the last one.
@@ -63,10 +83,13 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     constexpr int E = 16 / (int)sizeof(T);       // tokens of a 16-byte piece
     constexpr int STAGE = 8 * E;                 // tokens of a stage
     constexpr int XB = CKPT ? STAGE : kRowBytes; // bytes of a row of X
+    constexpr int GH = kRowBytes / 2, XH = XB / 2; // of half a stage
+    constexpr int X_AREA = GS * kRowBytes, S_AREA = X_AREA + XS * XB;
     constexpr int XL = XB / 16;                  // lanes that load it
     constexpr int GR = kThreads / 8, XR = kThreads / XL; // rows at once
     constexpr int PG = (GS + GR - 1) / GR, PX = (XS + XR - 1) / XR; // loads per lane
     static_assert(XS <= kThreads, "a lane per row for the exponents");
+    static_assert(X_AREA % XH == 0, "an exponent's place follows from its row's");
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
@@ -81,107 +104,115 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     const int32_t *reg = a.regions + 8 * (pair % a.n_regions);
     const int first = reg[0], tiles = reg[1], g_slots = reg[3], x_slots = reg[4] - reg[3];
     const int32_t *rows = a.rows + reg[2];
-    const uint32_t x_area = (uint32_t)a.slots_g * kRowBytes, s_area = x_area + (uint32_t)a.slots_x * XB;
 
     const int all = (int)(((int64_t)a.N + STAGE - 1) / STAGE), full = a.N / STAGE;
     const int s0 = split * a.per_split, s1 = split == a.splits - 1 ? all : s0 + a.per_split, f1 = min(s1, full);
 
     // this lane's rows: pass i takes row list entries i GR + thread / 8 (of X: i XR + thread / XL), at a place a constant further on
-    int64_t go[PG], xo[PX];
+    uint32_t g_row[PG], x_row[PX];               // (their numbers: addresses of 64 bits for all of them would be spilled)
     const uint32_t gq = threadIdx.x % 8, xq = threadIdx.x % XL;
     const int gr = (int)threadIdx.x / 8, xr = (int)threadIdx.x / XL;
+    const int64_t g_pitch = a.ldg * (int)sizeof(T), x_pitch = a.ldx * (CKPT ? 1 : (int)sizeof(T));
     const char *gbase = static_cast<const char *>(a.G) + (int64_t)s0 * kRowBytes, *xbase = static_cast<const char *>(a.X) + (int64_t)s0 * XB;
-    const uint32_t gu = place<kRowBytes>((uint32_t)gr, gq), xu = x_area + place<XB>((uint32_t)xr, xq);
+    auto g_piece = [&](int i) {
+        asm volatile("" : "+v"(g_row[i]));
+        return gbase + ((int64_t)g_row[i] * g_pitch + 16 * gq);
+    };
+    auto x_piece = [&](int i) {
+        asm volatile("" : "+v"(x_row[i]));
+        return xbase + ((int64_t)x_row[i] * x_pitch + 16 * xq);
+    };
+    auto g_place = [](uint32_t slot, uint32_t q) { return q / 4 * (GS * GH) + place<GH>(slot, q % 4); };
+    auto x_place = [](uint32_t slot, uint32_t q) { return X_AREA + q / (XL / 2) * (XS * XH) + place<XH>(slot, q % (XL / 2)); };
+    const uint32_t gu = g_place((uint32_t)gr, gq), xu = x_place((uint32_t)xr, xq);
     static_assert(GR % 16 == 0 && XR % 16 == 0, "the rows of two passes differ by a multiple of 16: their places by a constant");
 #pragma unroll
     for (int i = 0; i < PG; ++i)
-        go[i] = (int64_t)rows[min(i * GR + gr, g_slots - 1)] * a.ldg * (int)sizeof(T) + 16 * gq;
+        g_row[i] = (uint32_t)rows[min(i * GR + gr, g_slots - 1)];
 #pragma unroll
     for (int i = 0; i < PX; ++i)
-        xo[i] = (int64_t)rows[g_slots + min(i * XR + xr, x_slots - 1)] * a.ldx * (CKPT ? 1 : (int)sizeof(T)) + 16 * xq;
-    // exponents: lane r has 16 neighbouring ones of row r, from group `window` on
+        x_row[i] = (uint32_t)rows[g_slots + min(i * XR + xr, x_slots - 1)];
+    // exponents: lane r has up to 16 neighbouring ones of row r, the next stage's first
+    constexpr int SG = STAGE / 32;               // groups of a stage: 2 or 1
     const int groups = (int)(((int64_t)a.N + 31) / 32);
-    const uint8_t *sp = nullptr;
-    int window = 0;
-    uint4v exps = {0u, 0u, 0u, 0u};
-    auto fetch_exps = [&](int group) {
-        window = max(0, min(group, groups - 16));
-        if (groups >= 16) {
-            __builtin_memcpy(&exps, sp + window, 16);
+    [[maybe_unused]] const uint8_t *sp = nullptr;
+    [[maybe_unused]] uint4v exps = {0u, 0u, 0u, 0u};
+    [[maybe_unused]] int have = 0;               // stages that are left in them
+    [[maybe_unused]] auto fetch_exps = [&](int s) {
+        const int group = s * SG;
+        if (group + 16 <= groups) {
+            __builtin_memcpy(&exps, sp + group, 16);
         } else {
-            exps = uint4v{0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int k = 0; k < 15; ++k)
-                if (k < groups) exps[k / 4] |= (uint32_t)sp[k] << (8 * (k & 3));
+            exps = first_of(sp + group, groups - group);
         }
+        have = 16 / SG;
     };
-    auto put_exps = [&](int s) {
-        // (the two groups of 64 tokens, or the one of 32)
-        const int first_group = (int)((int64_t)s * STAGE / 32), k = first_group - window;
-        const uint32_t lo = k < 8 ? (k < 4 ? exps[0] : exps[1]) : (k < 12 ? exps[2] : exps[3]);
-        const uint32_t hi = k + 1 < 8 ? (k + 1 < 4 ? exps[0] : exps[1]) : (k + 1 < 12 ? exps[2] : exps[3]);
-        const uint32_t b0 = (lo >> (8 * (k & 3))) & 0xffu, b1 = STAGE == 64 && first_group + 1 < groups ? (hi >> (8 * ((k + 1) & 3))) & 0xffu : b0;
-        if ((int)threadIdx.x < x_slots) *reinterpret_cast<uint16_t *>(smem + s_area + 2 * threadIdx.x) = (uint16_t)(b0 | b1 << 8);
+    // a stage's exponents as the floats that conversions take, two for each row
+    [[maybe_unused]] auto put_exps = [&]() {
+        const uint32_t b0 = exps[0] & 0xffu, b1 = SG == 2 ? (exps[0] >> 8) & 0xffu : b0;
+        if ((int)threadIdx.x < x_slots) *reinterpret_cast<uint2v *>(smem + S_AREA + 8 * threadIdx.x) = uint2v{b0 << 23, b1 << 23};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) exps[k] = exps[k] >> (8 * SG) | (k < 3 ? exps[k < 3 ? k + 1 : 3] << (32 - 8 * SG) : 0u);
+        --have;
     };
     if constexpr (CKPT) {
         sp = a.S + (int64_t)rows[g_slots + min((int)threadIdx.x, x_slots - 1)] * a.lds;
-        fetch_exps((int)((int64_t)s0 * STAGE / 32));
+        fetch_exps(s0);
     }
 
     uint4v hg[PG], hx[PX];
     if (s0 < f1) {
 #pragma unroll
         for (int i = 0; i < PG; ++i)
-            if (i * GR < g_slots) __builtin_memcpy(&hg[i], gbase + go[i], 16);
+            if (i * GR < g_slots) __builtin_memcpy(&hg[i], g_piece(i), 16);
 #pragma unroll
         for (int i = 0; i < PX; ++i)
-            if (i * XR < x_slots) __builtin_memcpy(&hx[i], xbase + xo[i], 16);
+            if (i * XR < x_slots) __builtin_memcpy(&hx[i], x_piece(i), 16);
     }
 
-    // ---- this wavefront's tiles
+    // ---- this wavefront's tiles: places of this lane's pieces of the first half
     const int per = (tiles + kGradWaves - 1) / kGradWaves;
     const int my0 = wave * per, mine = min(per, tiles - my0);
-    uint32_t ops[TILES];                         // of this lane's piece: 16-byte unit in the rows of G | place in those of X << 16
+    uint32_t pa[TILES], pb[TILES], fresh = 0;    // (bit t: tile t's rows of G are not those of tile t - 1)
     float4v acc[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
         const uint32_t o = t < mine ? a.ops[(int64_t)(first + my0 + t) * 16 + n] : (uint32_t)g_slots << 16;
         const uint32_t x = (o >> 16) - (uint32_t)g_slots;
-        const uint32_t to = CKPT ? place<XB>(x, g * E / 16) + g * E % 16 : place<XB>(x, g) / 16;
-        ops[t] = place<kRowBytes>(o & 0xffffu, g) / 16 | to << 16;
+        pa[t] = place<GH>(o & 0xffffu, g);
+        pb[t] = X_AREA + (CKPT ? place<XH>(x, g * E / 16) + g * E % 16 : place<XH>(x, g));
+        if (t == 0 || __builtin_amdgcn_readfirstlane(pa[t]) != __builtin_amdgcn_readfirstlane(pa[t > 0 ? t - 1 : 0])) fresh |= 1u << t;
         acc[t] = float4v{0.f, 0.f, 0.f, 0.f};
     }
     auto multiply = [&]() {
+        uint4v x[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            struct Operands {
-                uint4v x;
-                uint32_t y[CKPT ? E / 4 : 4], e;
-            };
-            Operands o[2];
-            auto load = [&](int t) {
-                Operands &p = o[t & 1];
-                asm volatile("" : "+v"(ops[t])); // (addresses are worked out here: kept for all tiles they are spilled)
-                p.x = *reinterpret_cast<const uint4v *>(smem + (((ops[t] & 0xffffu) ^ (4u * u)) << 4));
-                const uint32_t to = CKPT ? (ops[t] >> 16) ^ (XB / 2u * u) : ((ops[t] >> 16) ^ (4u * u)) << 4;
-                __builtin_memcpy(p.y, __builtin_assume_aligned(smem + x_area + to, CKPT ? E : 16), sizeof p.y);
-                if constexpr (CKPT) p.e = *reinterpret_cast<const uint8_t *>(smem + s_area + (to / XB) * 2u + u);
-            };
-            load(0);
+        for (int t = 0; t < TILES; ++t) {
+            if (t >= mine) break;
+            if (fresh >> t & 1u) {
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) {
-                if (t >= mine) break;
-                if (t + 1 < TILES) load(t + 1);
-                const Operands &p = o[t & 1];
+                for (int u = 0; u < 2; ++u) x[u] = *reinterpret_cast<const uint4v *>(smem + pa[t] + u * (GS * GH));
+            }
+            uint32_t c[2][CKPT ? E / 4 : 4];
+            [[maybe_unused]] uint2v e;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) __builtin_memcpy(c[u], __builtin_assume_aligned(smem + pb[t] + u * (XS * XH), CKPT ? E : 16), sizeof c[u]);
+            if constexpr (CKPT) {
+                uint32_t row = pb[t];
+                asm volatile("" : "+v"(row)); // (or the addresses of all tiles are kept in registers that there are not)
+                e = *reinterpret_cast<const uint2v *>(smem + (row / XH * 8u + (S_AREA - X_AREA / XH * 8)));
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
                 uint4v y;
                 if constexpr (CKPT) {
                     T w[E];
-                    e4m3_to<T, E>(p.y, p.e, w);
+                    e4m3_to<T, E>(c[u], __builtin_bit_cast(float, (uint32_t)e[u]), w);
                     __builtin_memcpy(&y, w, 16);
                 } else {
-                    __builtin_memcpy(&y, p.y, 16);
+                    __builtin_memcpy(&y, c[u], 16);
                 }
-                acc[t] = product<T>(p.x, y, acc[t]);
+                acc[t] = product<T>(x[u], y, acc[t]);
             }
         }
     };
@@ -189,9 +220,8 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     for (int s = s0; s < f1; ++s) {
         if (s > s0) lds_barrier();               // (all of the stage before has been read; loads stay in flight)
         if constexpr (CKPT) {
-            put_exps(s);
-            const int next = (int)((int64_t)(s + 1) * STAGE / 32);
-            if (s + 1 < all && next + STAGE / 32 > window + 16) fetch_exps(next);
+            put_exps();
+            if (have == 0 && s + 1 < s1) fetch_exps(s + 1);
         }
         const bool more = s + 1 < f1;
         gbase += kRowBytes;
@@ -199,14 +229,14 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
 #pragma unroll
         for (int i = 0; i < PG; ++i) {
             if (i * GR >= g_slots) continue;
-            if (i * GR + gr < g_slots) *reinterpret_cast<uint4v *>(smem + gu + i * (GR * kRowBytes)) = hg[i];
-            if (more) __builtin_memcpy(&hg[i], gbase + go[i], 16);
+            if (i * GR + gr < g_slots) *reinterpret_cast<uint4v *>(smem + gu + i * (GR * GH)) = hg[i];
+            if (more) __builtin_memcpy(&hg[i], g_piece(i), 16);
         }
 #pragma unroll
         for (int i = 0; i < PX; ++i) {
             if (i * XR >= x_slots) continue;
-            if (i * XR + xr < x_slots) *reinterpret_cast<uint4v *>(smem + xu + i * (XR * XB)) = hx[i];
-            if (more) __builtin_memcpy(&hx[i], xbase + xo[i], 16);
+            if (i * XR + xr < x_slots) *reinterpret_cast<uint4v *>(smem + xu + i * (XR * XH)) = hx[i];
+            if (more) __builtin_memcpy(&hx[i], x_piece(i), 16);
         }
         lds_barrier();
         multiply();
@@ -215,31 +245,20 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
         // the stage behind the last full one, in the last range
         const int n0 = full * STAGE;
         __syncthreads();
-        if constexpr (CKPT) put_exps(full);
+        if constexpr (CKPT) put_exps();
         for (int p = threadIdx.x; p < (g_slots + (CKPT ? 0 : x_slots)) * 8; p += kThreads) {
             const int slot = p / 8, q = p % 8;
             const bool in_g = slot < g_slots;
             const T *src = in_g ? static_cast<const T *>(a.G) + (int64_t)rows[slot] * a.ldg : static_cast<const T *>(a.X) + (int64_t)rows[slot] * a.ldx;
-            T w[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                w[e] = (T)0.f;
-                if (n0 + q * E + e < a.N) w[e] = src[n0 + q * E + e];
-            }
-            uint4v o;
-            __builtin_memcpy(&o, w, 16);
-            *reinterpret_cast<uint4v *>(smem + (in_g ? place<kRowBytes>((uint32_t)slot, (uint32_t)q)
-                                                     : x_area + place<kRowBytes>((uint32_t)(slot - g_slots), (uint32_t)q))) = o;
+            const uint4v o = first_of(src + n0 + q * E, a.N - n0 - q * E);
+            *reinterpret_cast<uint4v *>(smem + (in_g ? g_place((uint32_t)slot, (uint32_t)q) : x_place((uint32_t)(slot - g_slots), (uint32_t)q))) = o;
         }
         if constexpr (CKPT)
             for (int p = threadIdx.x; p < x_slots * XL; p += kThreads) {
                 const int slot = p / XL, q = p % XL, col = n0 + q * 16;
                 const uint8_t *src = static_cast<const uint8_t *>(a.X) + (int64_t)rows[g_slots + slot] * a.ldx;
-                uint4v codes = {0u, 0u, 0u, 0u};
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (col + e < a.N) codes[e / 4] |= (uint32_t)src[col + e] << (8 * (e & 3));
-                *reinterpret_cast<uint4v *>(smem + x_area + place<XB>((uint32_t)slot, (uint32_t)q)) = codes;
+                const uint4v codes = first_of(src + col, a.N - col);
+                *reinterpret_cast<uint4v *>(smem + x_place((uint32_t)slot, (uint32_t)q)) = codes;
             }
         __syncthreads();
         multiply();
@@ -275,7 +294,8 @@ template <typename T, bool CKPT, int SHAPE> ubp_status launch_one(GradArgs a, hi
     if (grid * kThreads >= (int64_t(1) << 32)) return UBP_ERR_UNSUPPORTED; // (a launch's threads are counted in 32 bits)
     static_assert(kGradUnit % STAGE == 0, "a range is whole stages");
     a.per_split /= STAGE;
-    const size_t lds = (size_t)a.slots_g * kRowBytes + (size_t)a.slots_x * (CKPT ? STAGE + 2 : kRowBytes);
+    constexpr size_t lds = (size_t)S.g_slots * kRowBytes + (size_t)S.x_slots * (CKPT ? STAGE + 8 : kRowBytes);
+    static_assert(lds <= 160 * 1024, "a stage fits LDS");
     return launch_kernel(kernel, dim3((unsigned)grid), dim3(kThreads), lds, st, a);
 }
 

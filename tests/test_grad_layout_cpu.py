@@ -40,7 +40,7 @@ int main(int argc, char **argv) {
     CHECK(L.usable && L.built);
     CHECK((int64_t)L.ops.size() == L.n_tiles * 16 && (int64_t)L.inv.size() == L.n_tiles * 256 && (int)L.regions.size() == 8 * L.n_regions);
     const ubp::GradShape S = ubp::kGradShapes[L.shape];
-    CHECK(L.max_tiles <= S.tiles && L.max_g <= S.g_slots && L.max_x <= S.x_slots && L.max_slots <= ubp::kGradSlots);
+    CHECK(L.max_tiles <= S.tiles && L.max_g <= S.g_slots && L.max_x <= S.x_slots);
     std::vector<int32_t> start((size_t)nb);
     for (int r = 0; r + bh <= M; ++r)
         for (int32_t b = p->indptr[(size_t)r]; b < p->indptr[(size_t)r + 1]; ++b) start[(size_t)b] = r;
