@@ -225,7 +225,7 @@ constexpr int kGradMinTokens = 2 * kGradUnit;
 // Tiles a wavefront keeps and LDS rows for G and for X of a region, at most, per instantiation of the kernel.
 struct GradShape { int tiles, g_slots, x_slots; };
 constexpr int kNumGradShapes = 3;
-constexpr GradShape kGradShapes[kNumGradShapes] = {{2, 256, 256}, {4, 384, 384}, {8, 640, 640}};
+constexpr GradShape kGradShapes[kNumGradShapes] = {{2, 256, 256}, {4, 384, 384}, {8, 624, 624}};
 constexpr GradShape kGradLargest = kGradShapes[kNumGradShapes - 1];
 
 // Host image of the weight gradient's layout.  A tile is the product of 16 consecutive rows of G with 16 rows of X; a region

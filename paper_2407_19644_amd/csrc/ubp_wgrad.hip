@@ -84,7 +84,9 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     constexpr int STAGE = 8 * E;                 // tokens of a stage
     constexpr int XB = CKPT ? STAGE : kRowBytes; // bytes of a row of X
     constexpr int GH = kRowBytes / 2, XH = XB / 2; // of half a stage
-    constexpr int X_AREA = GS * kRowBytes, S_AREA = X_AREA + XS * XB;
+    // Halves lie 64 bytes more apart than their rows take: the 8 lanes that LDS serves together write one row's pieces of both
+    // halves (or two or four rows of codes), which would meet in the same banks.
+    constexpr int G_HALF = GS * GH + 64, X_HALF = XS * XH + 64, X_AREA = 2 * G_HALF, S_AREA = X_AREA + 2 * X_HALF;
     constexpr int XL = XB / 16;                  // lanes that load it
     constexpr int GR = kThreads / 8, XR = kThreads / XL; // rows at once
     constexpr int PG = (GS + GR - 1) / GR, PX = (XS + XR - 1) / XR; // loads per lane
@@ -122,8 +124,8 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
         asm volatile("" : "+v"(x_row[i]));
         return xbase + ((int64_t)x_row[i] * x_pitch + 16 * xq);
     };
-    auto g_place = [](uint32_t slot, uint32_t q) { return q / 4 * (GS * GH) + place<GH>(slot, q % 4); };
-    auto x_place = [](uint32_t slot, uint32_t q) { return X_AREA + q / (XL / 2) * (XS * XH) + place<XH>(slot, q % (XL / 2)); };
+    auto g_place = [&](uint32_t slot, uint32_t q) { return q / 4 * G_HALF + place<GH>(slot, q % 4); };
+    auto x_place = [&](uint32_t slot, uint32_t q) { return X_AREA + q / (XL / 2) * X_HALF + place<XH>(slot, q % (XL / 2)); };
     const uint32_t gu = g_place((uint32_t)gr, gq), xu = x_place((uint32_t)xr, xq);
     static_assert(GR % 16 == 0 && XR % 16 == 0, "the rows of two passes differ by a multiple of 16: their places by a constant");
 #pragma unroll
@@ -191,12 +193,12 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
             if (t >= mine) break;
             if (fresh >> t & 1u) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) x[u] = *reinterpret_cast<const uint4v *>(smem + pa[t] + u * (GS * GH));
+                for (int u = 0; u < 2; ++u) x[u] = *reinterpret_cast<const uint4v *>(smem + pa[t] + u * G_HALF);
             }
             uint32_t c[2][CKPT ? E / 4 : 4];
             [[maybe_unused]] uint2v e;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) __builtin_memcpy(c[u], __builtin_assume_aligned(smem + pb[t] + u * (XS * XH), CKPT ? E : 16), sizeof c[u]);
+            for (int u = 0; u < 2; ++u) __builtin_memcpy(c[u], __builtin_assume_aligned(smem + pb[t] + u * X_HALF, CKPT ? E : 16), sizeof c[u]);
             if constexpr (CKPT) {
                 uint32_t row = pb[t];
                 asm volatile("" : "+v"(row)); // (or the addresses of all tiles are kept in registers that there are not)
@@ -294,7 +296,7 @@ template <typename T, bool CKPT, int SHAPE> ubp_status launch_one(GradArgs a, hi
     if (grid * kThreads >= (int64_t(1) << 32)) return UBP_ERR_UNSUPPORTED; // (a launch's threads are counted in 32 bits)
     static_assert(kGradUnit % STAGE == 0, "a range is whole stages");
     a.per_split /= STAGE;
-    constexpr size_t lds = (size_t)S.g_slots * kRowBytes + (size_t)S.x_slots * (CKPT ? STAGE + 8 : kRowBytes);
+    constexpr size_t lds = 256 + (size_t)S.g_slots * kRowBytes + (size_t)S.x_slots * (CKPT ? STAGE + 8 : kRowBytes);
     static_assert(lds <= 160 * 1024, "a stage fits LDS");
     return launch_kernel(kernel, dim3((unsigned)grid), dim3(kThreads), lds, st, a);
 }
