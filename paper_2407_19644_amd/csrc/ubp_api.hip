@@ -590,6 +590,16 @@ ubp_status checkpoint(const ubp_packed *p, bool save, void *X, int64_t ldx, int3
     return save ? launch_save(a, p->dtype, stream) : launch_load(a, p->dtype, stream);
 }
 
+// (with p->lock held)
+GradRanges ranges_of(const ubp_packed *p, const GradLayout &L, int32_t N) {
+    GradLayoutDev &D = p->d_grad;
+    if (D.N != N) {
+        D.ranges = grad_ranges(L, N, (int)(kGradRowBytes / dtype_size(p->dtype)));
+        D.N = N;
+    }
+    return D.ranges;
+}
+
 ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const void *X, int64_t ldx, const uint8_t *S, int64_t lds, bool saved,
                        int32_t N, float *dvalues, int32_t accumulate, void *workspace, int64_t workspace_bytes, void *stream, bool dry) try {
     if (!p || p->device == UBP_HOST_ONLY || N < 0) return UBP_ERR_INVALID_ARG;
@@ -602,12 +612,14 @@ ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const vo
     DeviceGuard guard(p->device);
     if (!guard.ok) return UBP_ERR_DEVICE;
     const GradLayout *L = nullptr;
+    GradRanges ranges = {1, kGradUnit};
     {
         std::lock_guard<std::mutex> hold(p->lock);
         L = &get_grad_layout(p);
         if (!L->usable) return UBP_ERR_UNSUPPORTED;
         const ubp_status rc = upload_grad_layout(p);
         if (rc != UBP_OK) return rc;
+        if (N > 0) ranges = ranges_of(p, *L, N);
     }
     GradArgs a = {};
     a.regions = p->d_grad.regions;
@@ -622,6 +634,8 @@ ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const vo
     a.lds = lds;
     a.N = N;
     a.n_regions = L->n_regions;
+    a.slots_g = L->max_g;
+    a.slots_x = L->max_x;
     a.n_tiles = L->n_tiles;
     a.out = dvalues;
     a.accumulate = accumulate ? 1 : 0;
@@ -634,7 +648,6 @@ ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const vo
         if (accumulate) return UBP_OK;
         return launch_weight_sum(a, stream); // (a sum of no ranges)
     }
-    const GradRanges ranges = grad_ranges(*L, N);
     a.splits = ranges.splits;
     a.per_split = ranges.tokens;
     if (a.splits > 1) {
@@ -714,7 +727,7 @@ int64_t ubp_weight_grad_workspace(const ubp_packed *p, int32_t N) {
         std::lock_guard<std::mutex> hold(p->lock);
         const ubp::GradLayout &L = ubp::get_grad_layout(p);
         if (!L.usable) return -1;
-        const int splits = ubp::grad_ranges(L, N).splits;
+        const int splits = ubp::ranges_of(p, L, N).splits;
         return splits > 1 ? splits * L.n_tiles * 1024 : 0;
     } catch (...) {
         return -1;

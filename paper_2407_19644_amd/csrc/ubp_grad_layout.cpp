@@ -172,6 +172,11 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
     out.ops.resize((size_t)n * 16);
     std::vector<int32_t> slot_x((size_t)p->K, 0);
     for (const Region &r : done) {
+        out.max_g = std::max(out.max_g, (int)r.rows.g);
+        out.max_x = std::max(out.max_x, (int)r.rows.x);
+    }
+    out.rows.reserve(done.size() * (size_t)(out.max_g + out.max_x));
+    for (const Region &r : done) {
         int32_t *o = &order[(size_t)r.first];
         // tiles of one window side by side
         std::sort(o, o + r.n, [&](int32_t a, int32_t b) {
@@ -179,13 +184,12 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
             return s.r0 != t.r0 ? s.r0 < t.r0 : s.col[0] < t.col[0];
         });
         union_of(tiles, o, r.n, g, x);
-        const int32_t first_slot = (int32_t)out.rows.size();
-        const int32_t g_slots = (int32_t)padded(g.size()), all = g_slots + (int32_t)padded(x.size());
+        const size_t first_row = out.rows.size();
         for (int32_t v : g) out.rows.push_back(std::min(v, p->M - 1));
-        out.rows.resize((size_t)first_slot + (size_t)g_slots, out.rows.back());
-        for (size_t k = 0; k < x.size(); ++k) slot_x[(size_t)x[k]] = g_slots + (int32_t)k;
+        out.rows.resize(first_row + (size_t)out.max_g, out.rows.back());
+        for (size_t k = 0; k < x.size(); ++k) slot_x[(size_t)x[k]] = (int32_t)k;
         out.rows.insert(out.rows.end(), x.begin(), x.end());
-        out.rows.resize((size_t)first_slot + (size_t)all, out.rows.back());
+        out.rows.resize(first_row + (size_t)(out.max_g + out.max_x), out.rows.back());
         for (int64_t t = 0; t < r.n; ++t) {
             const Tile &a = tiles[(size_t)o[t]];
             const int64_t to = r.first + t;
@@ -194,11 +198,8 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
                 out.ops[(size_t)(to * 16 + k)] = (uint32_t)(g0 + k) | (uint32_t)slot_x[(size_t)a.col[k < a.n ? k : 0]] << 16;
             std::copy(&inv[(size_t)o[t] * 256], &inv[(size_t)o[t] * 256] + 256, &out.inv[(size_t)to * 256]);
         }
-        out.regions.insert(out.regions.end(), {(int32_t)r.first, (int32_t)r.n, first_slot, g_slots, all, 0, 0, 0});
+        out.regions.insert(out.regions.end(), {(int32_t)r.first, (int32_t)r.n, (int32_t)r.rows.g, (int32_t)r.rows.x});
         out.max_tiles = std::max(out.max_tiles, (int)((r.n + kGradWaves - 1) / kGradWaves));
-        out.max_g = std::max(out.max_g, (int)g_slots);
-        out.max_x = std::max(out.max_x, (int)(all - g_slots));
-        out.max_slots = std::max(out.max_slots, (int)all);
     }
     while (out.max_tiles > kGradShapes[out.shape].tiles || out.max_g > kGradShapes[out.shape].g_slots || out.max_x > kGradShapes[out.shape].x_slots)
         ++out.shape; // (the largest holds them)
@@ -207,13 +208,24 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
     return L;
 }
 
-// The regions of all ranges fill the CUs about once, and a range has kGradMinTokens tokens at least.
-GradRanges grad_ranges(const GradLayout &L, int64_t N) {
-    const int64_t fill = L.n_regions ? std::max<int64_t>(1, kGradWorkgroups / L.n_regions) : 1;
+// As many ranges as take the least time by an estimate in stages (0.8 us each at 4 tiles a wavefront, more at 8): rounds of
+// workgroups, each of them its range's stages and about 12 for its lists, its first loads and its sums' way out; and with more
+// than one range a launch, worth 5, that reads and writes 1 KB per tile and range, 2000 of them in the time of a stage.
+GradRanges grad_ranges(const GradLayout &L, int64_t N, int stage_tokens) {
     const int64_t units = std::max<int64_t>(1, N / kGradUnit);             // (a short unit belongs to the last range)
-    const int64_t most = std::max<int64_t>(1, std::min(fill, N / kGradMinTokens));
-    const int64_t each = (units + most - 1) / most;
-    return {(int)((units + each - 1) / each), (int)(each * kGradUnit)};    // (none of them empty)
+    const double stages = (double)N / stage_tokens;
+    int64_t best_each = units;
+    double best = 0.0;
+    for (int64_t s = 1; s <= std::min<int64_t>(units, kGradWorkgroups); ++s) {
+        const int64_t each = (units + s - 1) / s, ranges = (units + each - 1) / each; // (none of them empty)
+        const double rounds = (double)((L.n_regions * ranges + kGradWorkgroups - 1) / kGradWorkgroups);
+        const double t = rounds * (stages * (double)each / (double)units + 12.0) + (ranges > 1 ? 5.0 + (double)(ranges * L.n_tiles) / 2000.0 : 0.0);
+        if (s == 1 || t < best) {
+            best = t;
+            best_each = each;
+        }
+    }
+    return {(int)((units + best_each - 1) / best_each), (int)(best_each * kGradUnit)};
 }
 
 } // namespace ubp

@@ -216,23 +216,26 @@ struct Wros4Layout {
 };
 
 // Weight gradient: wavefronts of a workgroup, regions that a layer is cut into where its tiles allow, workgroups that fill
-// the card, tokens of a range at least and its unit.
+// the card, bytes of a row that a stage takes, tokens that a range is a multiple of.
 constexpr int kGradWaves = 16;
 constexpr int kGradRegions = 32;
 constexpr int kGradWorkgroups = 256;
+constexpr int kGradRowBytes = 128;
 constexpr int kGradUnit = 64;
-constexpr int kGradMinTokens = 2 * kGradUnit;
 // Tiles a wavefront keeps and LDS rows for G and for X of a region, at most, per instantiation of the kernel.
 struct GradShape { int tiles, g_slots, x_slots; };
 constexpr int kNumGradShapes = 3;
 constexpr GradShape kGradShapes[kNumGradShapes] = {{2, 256, 256}, {4, 384, 384}, {8, 624, 624}};
 constexpr GradShape kGradLargest = kGradShapes[kNumGradShapes - 1];
 
+// Ranges that the sum over the tokens is cut into, and the tokens of each (the last one takes what is left).
+struct GradRanges { int splits, tokens; };
+
 // Host image of the weight gradient's layout.  A tile is the product of 16 consecutive rows of G with 16 rows of X; a region
 // is a run of tiles that one workgroup keeps in registers, with the rows of G and X that they need.
-//   regions : 8 words each: first tile, tiles, first entry of rows, entries for G (a multiple of 16), for G and X (likewise)
-//   rows    : row of G, then of X, per LDS row of the region (rows that fill up 16 repeat the last one)
-//   ops     : 16 words per tile: LDS row of G | LDS row of X << 16
+//   regions : 4 words each: first tile, tiles, LDS rows of G, of X (multiples of 16)
+//   rows    : max_g + max_x words each: the row of G per LDS row of G, then of X (what fills up a list repeats its last one)
+//   ops     : 16 words per tile: LDS row of G | of X << 16
 //   inv     : 256 words per tile: the value that element (16 (i / 4) + j) 4 + i % 4, row i and column j of the tile,
 //             is the gradient of (a place in the canonical values), -1 for none.  Every value appears once.
 struct GradLayout {
@@ -240,7 +243,7 @@ struct GradLayout {
     int64_t n_tiles = 0;
     int n_regions = 0;
     int max_tiles = 0;                   // of a wavefront
-    int max_g = 0, max_x = 0, max_slots = 0; // LDS rows of a region
+    int max_g = 0, max_x = 0;            // LDS rows of a region
     int shape = 0;                       // the smallest of kGradShapes that holds them
     std::vector<int32_t> regions, rows, inv;
     std::vector<uint32_t> ops;
@@ -275,6 +278,8 @@ struct GradLayoutDev {
     int32_t *regions = nullptr, *rows = nullptr, *inv = nullptr;
     uint32_t *ops = nullptr;
     bool uploaded = false;
+    int32_t N = 0;            // the last number of tokens whose ranges were worked out (which takes 1.5 us), and they
+    GradRanges ranges{1, kGradUnit};
 };
 struct TileLayoutDev {
     uint16_t *frags = nullptr;
@@ -397,6 +402,7 @@ struct GradArgs {
     const uint8_t *S;         // the checkpoint's exponents
     int64_t ldg, ldx, lds;
     int N, n_regions, splits;
+    int slots_g, slots_x;     // lengths of a region's lists of rows
     int per_split;            // tokens of a range (in the kernel: stages); the last one takes what is left
     int64_t n_tiles;
     float *out;               // dvalues
@@ -500,9 +506,7 @@ const TileLayout &get_tile_layout(const ubp_packed *p);
 const DirectLayout &get_direct_layout(const ubp_packed *p);
 const Wros4Layout &get_wros4_layout(const ubp_packed *p);
 const GradLayout &get_grad_layout(const ubp_packed *p);
-// Ranges that the sum over N tokens is cut into, and the tokens of each (the last one takes what is left).
-struct GradRanges { int splits, tokens; };
-GradRanges grad_ranges(const GradLayout &L, int64_t N);
+GradRanges grad_ranges(const GradLayout &L, int64_t N, int stage_tokens);
 const MaskStats &get_mask_stats(const ubp_packed *p);
 // Stripes per wavefront of the gather kernel.  They follow the block height: a 16-row block touches two stripes
 // anyway, so tall row groups cost little extra zero fill and divide the staging of X by the rows a workgroup

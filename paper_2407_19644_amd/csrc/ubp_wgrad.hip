@@ -8,7 +8,7 @@ namespace ubp {
 
 namespace {
 
-constexpr int kRowBytes = 128; // of a row of G or X that a stage takes: 64 16-bit or 32 fp32 tokens, a cache line
+constexpr int kRowBytes = kGradRowBytes; // of a row of G or X that a stage takes: 64 16-bit or 32 fp32 tokens, a cache line
 constexpr int kThreads = 64 * kGradWaves;
 
 // A stage lies in LDS in two halves, each with rows of BYTES bytes: 64 of G and X, 32 or 16 of a checkpoint's codes.  Place of
@@ -103,9 +103,11 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     const int64_t pair = (pairs * xcd >> 3) + (blockIdx.x >> 3);
     if (pair >= (pairs * (xcd + 1) >> 3)) return;
     const int split = (int)(pair / a.n_regions);
-    const int32_t *reg = a.regions + 8 * (pair % a.n_regions);
-    const int first = reg[0], tiles = reg[1], g_slots = reg[3], x_slots = reg[4] - reg[3];
-    const int32_t *rows = a.rows + reg[2];
+    const int region = (int)(pair % a.n_regions);
+    const int32_t *reg = a.regions + 4 * region;
+    const int first = reg[0], tiles = reg[1], g_slots = reg[2], x_slots = reg[3];
+    // (lists of one length, filled up with some row: to read them takes nothing but the region's number)
+    const int32_t *rows_g = a.rows + (int64_t)region * (a.slots_g + a.slots_x), *rows_x = rows_g + a.slots_g;
 
     const int all = (int)(((int64_t)a.N + STAGE - 1) / STAGE), full = a.N / STAGE;
     const int s0 = split * a.per_split, s1 = split == a.splits - 1 ? all : s0 + a.per_split, f1 = min(s1, full);
@@ -130,10 +132,10 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     static_assert(GR % 16 == 0 && XR % 16 == 0, "the rows of two passes differ by a multiple of 16: their places by a constant");
 #pragma unroll
     for (int i = 0; i < PG; ++i)
-        g_row[i] = (uint32_t)rows[min(i * GR + gr, g_slots - 1)];
+        g_row[i] = (uint32_t)rows_g[min(i * GR + gr, a.slots_g - 1)];
 #pragma unroll
     for (int i = 0; i < PX; ++i)
-        x_row[i] = (uint32_t)rows[g_slots + min(i * XR + xr, x_slots - 1)];
+        x_row[i] = (uint32_t)rows_x[min(i * XR + xr, a.slots_x - 1)];
     // exponents: lane r has up to 16 neighbouring ones of row r, the next stage's first
     constexpr int SG = STAGE / 32;               // groups of a stage: 2 or 1
     const int groups = (int)(((int64_t)a.N + 31) / 32);
@@ -158,7 +160,7 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
         --have;
     };
     if constexpr (CKPT) {
-        sp = a.S + (int64_t)rows[g_slots + min((int)threadIdx.x, x_slots - 1)] * a.lds;
+        sp = a.S + (int64_t)rows_x[min((int)threadIdx.x, a.slots_x - 1)] * a.lds;
         fetch_exps(s0);
     }
 
@@ -179,8 +181,7 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     float4v acc[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
-        const uint32_t o = t < mine ? a.ops[(int64_t)(first + my0 + t) * 16 + n] : (uint32_t)g_slots << 16;
-        const uint32_t x = (o >> 16) - (uint32_t)g_slots;
+        const uint32_t o = t < mine ? a.ops[(int64_t)(first + my0 + t) * 16 + n] : 0u, x = o >> 16;
         pa[t] = place<GH>(o & 0xffffu, g);
         pb[t] = X_AREA + (CKPT ? place<XH>(x, g * E / 16) + g * E % 16 : place<XH>(x, g));
         if (t == 0 || __builtin_amdgcn_readfirstlane(pa[t]) != __builtin_amdgcn_readfirstlane(pa[t > 0 ? t - 1 : 0])) fresh |= 1u << t;
@@ -251,14 +252,14 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
         for (int p = threadIdx.x; p < (g_slots + (CKPT ? 0 : x_slots)) * 8; p += kThreads) {
             const int slot = p / 8, q = p % 8;
             const bool in_g = slot < g_slots;
-            const T *src = in_g ? static_cast<const T *>(a.G) + (int64_t)rows[slot] * a.ldg : static_cast<const T *>(a.X) + (int64_t)rows[slot] * a.ldx;
+            const T *src = in_g ? static_cast<const T *>(a.G) + (int64_t)rows_g[slot] * a.ldg : static_cast<const T *>(a.X) + (int64_t)rows_x[slot - g_slots] * a.ldx;
             const uint4v o = first_of(src + n0 + q * E, a.N - n0 - q * E);
             *reinterpret_cast<uint4v *>(smem + (in_g ? g_place((uint32_t)slot, (uint32_t)q) : x_place((uint32_t)(slot - g_slots), (uint32_t)q))) = o;
         }
         if constexpr (CKPT)
             for (int p = threadIdx.x; p < x_slots * XL; p += kThreads) {
                 const int slot = p / XL, q = p % XL, col = n0 + q * 16;
-                const uint8_t *src = static_cast<const uint8_t *>(a.X) + (int64_t)rows[g_slots + slot] * a.ldx;
+                const uint8_t *src = static_cast<const uint8_t *>(a.X) + (int64_t)rows_x[slot] * a.ldx;
                 const uint4v codes = first_of(src + col, a.N - col);
                 *reinterpret_cast<uint4v *>(smem + x_place((uint32_t)slot, (uint32_t)q)) = codes;
             }
@@ -278,7 +279,15 @@ __global__ __launch_bounds__(256) void weight_sum_kernel(GradArgs a) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= a.n_tiles * 64) return;
     float4v sum = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) sum += *reinterpret_cast<const float4v *>(a.part + ((int64_t)s * a.n_tiles * 64 + i) * 4);
+    // (8 at a time: one after the other, each would wait for memory)
+    for (int s = 0; s < a.splits; s += 8) {
+        float4v v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const float4v *>(a.part + ((int64_t)min(s + k, a.splits - 1) * a.n_tiles * 64 + i) * 4);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (s + k < a.splits) sum += v[k];
+    }
     const uint4v to = *reinterpret_cast<const uint4v *>(a.inv + i * 4);
 #pragma unroll
     for (int e = 0; e < 4; ++e)

@@ -38,33 +38,31 @@ int main(int argc, char **argv) {
     CHECK(ubp_pack(W.data(), dt, M, K, K, bh, bw, blocks.data(), nb, UBP_HOST_ONLY, &p) == UBP_OK);
     const ubp::GradLayout &L = ubp::get_grad_layout(p);
     CHECK(L.usable && L.built);
-    CHECK((int64_t)L.ops.size() == L.n_tiles * 16 && (int64_t)L.inv.size() == L.n_tiles * 256 && (int)L.regions.size() == 8 * L.n_regions);
+    CHECK((int64_t)L.ops.size() == L.n_tiles * 16 && (int64_t)L.inv.size() == L.n_tiles * 256 && (int)L.regions.size() == 4 * L.n_regions);
     const ubp::GradShape S = ubp::kGradShapes[L.shape];
     CHECK(L.max_tiles <= S.tiles && L.max_g <= S.g_slots && L.max_x <= S.x_slots);
     std::vector<int32_t> start((size_t)nb);
     for (int r = 0; r + bh <= M; ++r)
         for (int32_t b = p->indptr[(size_t)r]; b < p->indptr[(size_t)r + 1]; ++b) start[(size_t)b] = r;
     std::vector<char> seen((size_t)(nb * bh * bw), 0);
-    int64_t next_tile = 0, next_row = 0;
+    int64_t next_tile = 0;
+    CHECK((int64_t)L.rows.size() == (int64_t)L.n_regions * (L.max_g + L.max_x));
     for (int g = 0; g < L.n_regions; ++g) {
-        const int32_t *R = &L.regions[(size_t)g * 8];
-        const int64_t first = R[0], tiles = R[1], rows = R[2], g_slots = R[3], slots = R[4];
-        CHECK(first == next_tile && tiles >= 1 && rows == next_row);
+        const int32_t *R = &L.regions[(size_t)g * 4], *rows_g = L.rows.data() + (size_t)g * (L.max_g + L.max_x), *rows_x = rows_g + L.max_g;
+        const int64_t first = R[0], tiles = R[1], g_slots = R[2], x_slots = R[3];
+        CHECK(first == next_tile && tiles >= 1);
         next_tile += tiles;
-        next_row += slots;
-        CHECK(g_slots % 16 == 0 && slots % 16 == 0 && g_slots < slots && slots <= L.max_slots && g_slots <= L.max_g && slots - g_slots <= L.max_x);
+        CHECK(g_slots > 0 && x_slots > 0 && g_slots % 16 == 0 && x_slots % 16 == 0 && g_slots <= L.max_g && x_slots <= L.max_x);
         CHECK((tiles + ubp::kGradWaves - 1) / ubp::kGradWaves <= L.max_tiles);
-        for (int64_t s = 0; s < slots; ++s) {
-            const int32_t row = L.rows[(size_t)(rows + s)];
-            CHECK(row >= 0 && row < (s < g_slots ? M : K));
-        }
+        for (int s = 0; s < L.max_g; ++s) CHECK(rows_g[s] >= 0 && rows_g[s] < M);
+        for (int s = 0; s < L.max_x; ++s) CHECK(rows_x[s] >= 0 && rows_x[s] < K);
         for (int64_t t = first; t < first + tiles; ++t) {
             int32_t gr[16], xr[16];
             for (int k = 0; k < 16; ++k) {
                 const uint32_t o = L.ops[(size_t)(t * 16 + k)];
-                CHECK((int64_t)(o & 0xffff) < g_slots && (int64_t)(o >> 16) >= g_slots && (int64_t)(o >> 16) < slots);
-                gr[k] = L.rows[(size_t)(rows + (o & 0xffff))];
-                xr[k] = L.rows[(size_t)(rows + (o >> 16))];
+                CHECK((int64_t)(o & 0xffff) < g_slots && (int64_t)(o >> 16) < x_slots);
+                gr[k] = rows_g[o & 0xffff];
+                xr[k] = rows_x[o >> 16];
             }
             for (int i = 0; i < 16; ++i)
                 for (int j = 0; j < 16; ++j) {
@@ -80,15 +78,15 @@ int main(int argc, char **argv) {
                 }
         }
     }
-    CHECK(next_tile == L.n_tiles && next_row == (int64_t)L.rows.size());
+    CHECK(next_tile == L.n_tiles);
     for (char c : seen) CHECK(c);
     for (int64_t n : {0, 1, 63, 64, 65, 127, 128, 129, 1567, 4096, 8192, 12543, 1 << 20, 0x7fffffff}) {
-        const ubp::GradRanges r = ubp::grad_ranges(L, n);
+        const ubp::GradRanges r = ubp::grad_ranges(L, n, dt == UBP_F32 ? 32 : 64);
         CHECK(r.splits >= 1 && r.splits <= 256 && r.tokens >= 64 && r.tokens % 64 == 0);
         CHECK(r.splits == 1 || (int64_t)(r.splits - 1) * r.tokens < n);
         CHECK((int64_t)r.splits * r.tokens + 63 >= n);
     }
-    std::printf("%lld tiles %d regions %d of a wavefront %d rows\n", (long long)L.n_tiles, L.n_regions, L.max_tiles, L.max_slots);
+    std::printf("%lld tiles %d regions %d of a wavefront %d + %d rows\n", (long long)L.n_tiles, L.n_regions, L.max_tiles, L.max_g, L.max_x);
     ubp_packed_free(p);
     return 0;
 }
