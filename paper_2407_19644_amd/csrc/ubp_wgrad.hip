@@ -33,24 +33,30 @@ template <> __device__ __forceinline__ float4v product<float>(uint4v a, uint4v b
     return c;
 }
 
-// The first `count` of the elements that 16 bytes hold, zeros behind them; nothing behind them is read.  (Where not all are
-// there, one by one, the last first: loads of all at once would take registers that the whole kernel then lacks.)
+// The first `count` of the elements that 16 bytes hold, zeros behind them; nothing behind them is read.  (Fewer bytes than 16
+// are 8, 4, 2 and 1 of them, side by side, as many loads at most and all in flight together: one element after the other, each
+// would wait for memory, which for 7 tokens took as long as 6 stages.)
 template <typename T> __device__ __forceinline__ uint4v first_of(const T *src, int count) {
-    constexpr int E = 16 / (int)sizeof(T), BITS = 8 * (int)sizeof(T);
     uint4v o = {0u, 0u, 0u, 0u};
-    if (count >= E) {
+    if (count >= 16 / (int)sizeof(T)) {
         __builtin_memcpy(&o, src, 16);
         return o;
     }
-#pragma unroll 1
-    for (int k = count - 1; k >= 0; --k) {
-        uint32_t v = 0u;
-        __builtin_memcpy(&v, src + k, sizeof(T));
-#pragma unroll
-        for (int w = 3; w >= 0; --w) o[w] = (BITS < 32 ? o[w] << (BITS & 31) : 0u) | (w > 0 ? o[w > 0 ? w - 1 : 0] >> ((32 - BITS) & 31) : 0u);
-        o[0] |= v;
-    }
-    return o;
+    const uint32_t c = (uint32_t)max(count, 0) * (uint32_t)sizeof(T);
+    const char *from = reinterpret_cast<const char *>(src);
+    uint64_t p8 = 0;
+    uint32_t p4 = 0;
+    uint16_t p2 = 0;
+    uint8_t p1 = 0;
+    if (c & 8u) __builtin_memcpy(&p8, from, 8);
+    if (c & 4u) __builtin_memcpy(&p4, from + (c & 8u), 4);
+    if (sizeof(T) < 4 && (c & 2u)) __builtin_memcpy(&p2, from + (c & 12u), 2);
+    if (sizeof(T) < 2 && (c & 1u)) p1 = (uint8_t)from[c & 14u];
+    uint64_t v = p1;
+    if (c & 2u) v = v << 16 | p2;
+    if (c & 4u) v = v << 32 | p4;
+    const uint64_t lo = c & 8u ? p8 : v, hi = c & 8u ? v : 0u;
+    return uint4v{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 
 // A tile's sums: of one range of several, or, where there is only one, at their places.
