@@ -527,8 +527,11 @@ ubp_status execute(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t 
 }
 
 // ------------------------------------------------------------------ training
+// Tokens of a call, at most: the kernels count columns, and run a workgroup's columns past the last one, in 32 bits.
+constexpr int32_t kMaxTokens = 0x7fffffff - 0xffff;
+
 // Workgroups of a row of the epilogue's gradient: one per row where the rows fill the card by themselves, else one per 4 chunks
-// (256 rows of 12544 tokens: see the kernel).
+// (sums of parts then meet in a second launch).
 int act_row_groups(int M, int N) {
     const int chunks = (int)(((int64_t)N + kActChunk - 1) / kActChunk);
     return M >= 1024 || chunks <= 4 ? 1 : (chunks + 3) / 4;
@@ -536,6 +539,7 @@ int act_row_groups(int M, int N) {
 
 ubp_status linear_grad(const ubp_packed *p, const void *dY, int64_t lddy, const void *Z, int64_t ldz, int32_t N, void *G, int64_t ldg,
                        float *dbias, int32_t activation, float lo, float hi, void *workspace, int64_t workspace_bytes, void *stream) {
+    if (p && N > kMaxTokens) return UBP_ERR_UNSUPPORTED;
     if (!p || p->device == UBP_HOST_ONLY || N < 0) return UBP_ERR_INVALID_ARG;
     if (activation < UBP_ACT_NONE || activation > UBP_ACT_SILU) return UBP_ERR_INVALID_ARG;
     if (activation == UBP_ACT_CLAMP && !(lo <= hi)) return UBP_ERR_INVALID_ARG;
@@ -572,6 +576,7 @@ ubp_status linear_grad(const ubp_packed *p, const void *dY, int64_t lddy, const 
 
 ubp_status checkpoint(const ubp_packed *p, bool save, void *X, int64_t ldx, int32_t N, uint8_t *Q, int64_t ldq, uint8_t *S, int64_t lds,
                       void *stream) {
+    if (p && N > kMaxTokens) return UBP_ERR_UNSUPPORTED;
     if (!p || p->device == UBP_HOST_ONLY || N < 0) return UBP_ERR_INVALID_ARG;
     if (N == 0) return UBP_OK;
     if (!X || !Q || !S || ldx < N || ldq < N || lds < ((int64_t)N + 31) / 32) return UBP_ERR_INVALID_ARG;
@@ -602,6 +607,7 @@ GradRanges ranges_of(const ubp_packed *p, const GradLayout &L, int32_t N) {
 
 ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const void *X, int64_t ldx, const uint8_t *S, int64_t lds, bool saved,
                        int32_t N, float *dvalues, int32_t accumulate, void *workspace, int64_t workspace_bytes, void *stream, bool dry) try {
+    if (p && N > kMaxTokens) return UBP_ERR_UNSUPPORTED;
     if (!p || p->device == UBP_HOST_ONLY || N < 0) return UBP_ERR_INVALID_ARG;
     if (!dry && p->nb == 0) return UBP_OK;
     if (!dry && !dvalues) return UBP_ERR_INVALID_ARG;
@@ -699,7 +705,7 @@ ubp_status ubp_linear(const ubp_packed *p, const void *X_dev, int64_t ldx, int32
 }
 
 int64_t ubp_linear_grad_workspace(const ubp_packed *p, int32_t N) {
-    if (!p || N < 0) return -1;
+    if (!p || N < 0 || N > ubp::kMaxTokens) return -1;
     const int groups = ubp::act_row_groups(p->M, N);
     return groups > 1 ? (int64_t)p->M * groups * 4 : 0;
 }
@@ -722,7 +728,7 @@ ubp_status ubp_checkpoint_load(const ubp_packed *p, const uint8_t *Q_dev, int64_
 }
 
 int64_t ubp_weight_grad_workspace(const ubp_packed *p, int32_t N) {
-    if (!p || N < 0) return -1;
+    if (!p || N < 0 || N > ubp::kMaxTokens) return -1;
     try {
         std::lock_guard<std::mutex> hold(p->lock);
         const ubp::GradLayout &L = ubp::get_grad_layout(p);

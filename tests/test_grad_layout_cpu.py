@@ -145,3 +145,22 @@ def test_refusals_without_a_device():
         assert e.value.code == 1
     with pytest.raises(KeyError):
         ubp.linear_grad(p, 64, 8, 64, 8, 8, 64, 8, activation="swish")
+
+
+def test_more_tokens_than_columns_can_be_counted():
+    """The kernels count columns in 32 bits, past the last one: refused before anything else about the call."""
+    from layer_util import layer
+    blocks, W, _ = layer(64, 48, 4, 4, 0.3, "f16", 1)
+    p = ubp.pack(W, "f16", 4, 4, blocks)
+    N = 2**31 - 2**16
+    assert ubp.weight_grad_workspace(p, N) > 0 and ubp.linear_grad_workspace(p, N) > 0
+    for n in (N + 1, 2**31 - 1):
+        for call in (lambda: ubp.weight_grad_workspace(p, n), lambda: ubp.linear_grad_workspace(p, n)):
+            with pytest.raises(ubp.UBPError):
+                call()
+        for call in (lambda: ubp.weight_grad(p, 64, n, 64, n, n, 64), lambda: ubp.weight_grad_checkpoint(p, 64, n, 64, n, 64, n, n, 64),
+                     lambda: ubp.linear_grad(p, 64, n, 64, n, n, 64, n, activation="silu"),
+                     lambda: ubp.checkpoint_save(p, 64, n, n, 64, n, 64, n), lambda: ubp.checkpoint_load(p, 64, n, 64, n, n, 64, n)):
+            with pytest.raises(ubp.UBPError) as e:
+                call()
+            assert e.value.code == 4
