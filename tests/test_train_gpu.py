@@ -492,3 +492,88 @@ def test_gradients_against_differences():
             diff = (f(Wd, b + e) - f(Wd, b - e)) / (2 * h)
             assert abs(db.cpu().numpy()[i] - diff) <= 2e-5 * np.abs(db.cpu().numpy()).max()
     p.free()
+
+
+# ------------------------------------------------------------------ far rows, calls at once
+@pytest.mark.parametrize("N", [70, 513])
+def test_rows_more_than_4_gigabytes_apart(N):
+    """All operators on matrices side by side in rows of 2^31 + 40 16-bit elements: the same bits as on narrow matrices."""
+    M = K = 2
+    dtype, pitch, G32 = "f16", 2**31 + 40, (N + 31) // 32
+    blocks, W, _ = layer(M, K, 2, 2, 1.0, dtype, seed=3)
+    p = ubp.pack(W, dtype, 2, 2, blocks, device=torch.cuda.current_device())
+    far = torch.empty(pitch + 16 * 1024, dtype=torch.float16, device=DEV)
+    mats = [to_device(make_activations(2, N, i, dtype, "normal"), dtype) for i in range(3)]
+
+    def run(place):
+        """place(i) -> (address, pitch in elements of 2 bytes) of matrix i."""
+        (x, ldx), (dy, ldd), (z, ldz), (g, ldg), (y, ldy), (xh, ldh), (q, ldq), (e, lde) = [place(i) for i in range(8)]
+        st = stream()
+        b, db, dv, dc = (torch.full((4,), 0.25, device=DEV) for _ in range(4))
+        n = ubp.weight_grad_workspace(p, N)
+        ws, wp = workspace(n)
+        ubp.linear(p, x, ldx, N, y, ldy, dtype, b.data_ptr(), "gelu", residual_ptr=dy, ldr=ldd, stream=st)
+        ubp.linear_grad(p, dy, ldd, z, ldz, N, g, ldg, db.data_ptr(), "gelu", stream=st)
+        ubp.checkpoint_save(p, x, ldx, N, q, 2 * ldq, e, 2 * lde, st)
+        ubp.checkpoint_load(p, q, 2 * ldq, e, 2 * lde, N, xh, ldh, st)
+        ubp.weight_grad(p, g, ldg, x, ldx, N, dv.data_ptr(), False, wp, n, st)
+        ubp.weight_grad_checkpoint(p, g, ldg, q, 2 * ldq, e, 2 * lde, N, dc.data_ptr(), False, wp, n, st)
+        torch.cuda.synchronize()
+        return db[:2], dv, dc
+
+    near = torch.zeros((8, 2, 1024), dtype=torch.float16, device=DEV)
+    for i, m in enumerate(mats):
+        near[i, :, :N] = m
+        for r in range(2):
+            far[r * pitch + 1024 * i:r * pitch + 1024 * i + N] = m[r]
+    want = run(lambda i: (near[i].data_ptr(), 1024))
+    got = run(lambda i: (far.data_ptr() + 2048 * i, pitch))
+    for u, v in zip(want, got):
+        assert torch.equal(u, v)
+    for i in (3, 4, 5):
+        for r in range(2):
+            assert torch.equal(near[i, r, :N], far[r * pitch + 1024 * i:r * pitch + 1024 * i + N])
+    bytes_of = lambda t, n: t.contiguous().view(torch.uint8)[:n]            # noqa: E731
+    for i, n in ((6, N), (7, G32)):
+        for r in range(2):
+            assert torch.equal(bytes_of(near[i, r], n), bytes_of(far[r * pitch + 1024 * i:r * pitch + 1024 * (i + 1)], n))
+    p.free()
+
+
+def test_two_streams_at_once():
+    """Weight gradients, the epilogue's gradients and checkpoints of one handle on two streams, with a workspace for each."""
+    M, K, N = 200, 180, 20000
+    blocks, W, _ = layer(M, K, 4, 4, 0.3, "bf16", seed=4)
+    p = ubp.pack(W, "bf16", 4, 4, blocks, device=torch.cuda.current_device())
+    nv, G32 = len(blocks) * 16, (N + 31) // 32
+    n, m = ubp.weight_grad_workspace(p, N), ubp.linear_grad_workspace(p, N)
+    assert n > 0 and m > 0
+    X, Y, Z = ([to_device(make_activations(r, N, 10 * i + r, "bf16", "normal"), "bf16") for i in range(2)] for r in (K, M, M + 1))
+
+    def buffers():
+        return (torch.zeros((M, N), dtype=torch.bfloat16, device=DEV), torch.zeros((K, N), dtype=torch.uint8, device=DEV),
+                torch.zeros((K, G32), dtype=torch.uint8, device=DEV), torch.zeros(M, device=DEV), torch.zeros(nv, device=DEV),
+                torch.zeros(n, dtype=torch.uint8, device=DEV), torch.zeros(m, dtype=torch.uint8, device=DEV))
+
+    def step(i, o, st):
+        g, q, e, db, dv, wn, wm = o
+        ubp.checkpoint_save(p, X[i].data_ptr(), N, N, q.data_ptr(), N, e.data_ptr(), G32, st)
+        ubp.linear_grad(p, Y[i].data_ptr(), N, Z[i].data_ptr(), N, N, g.data_ptr(), N, db.data_ptr(), "silu", workspace_ptr=wm.data_ptr(),
+                        workspace_bytes=m, stream=st)
+        for k in range(4):
+            ubp.weight_grad_checkpoint(p, g.data_ptr(), N, q.data_ptr(), N, e.data_ptr(), G32, N, dv.data_ptr(), k > 0, wn.data_ptr(), n, st)
+
+    want = [buffers(), buffers()]
+    for i in range(2):
+        step(i, want[i], stream())
+    torch.cuda.synchronize()
+    got, streams = [buffers(), buffers()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for i in range(2):
+        step(i, got[i], streams[i].cuda_stream)
+    torch.cuda.synchronize()
+    for u, v in zip(want, got):
+        for a, b in zip(u[:5], v[:5]):
+            assert torch.equal(a, b)
+    assert not torch.equal(got[0][4], got[1][4])
+    p.free()
