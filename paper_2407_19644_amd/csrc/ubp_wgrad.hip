@@ -142,7 +142,8 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
 #pragma unroll
     for (int i = 0; i < PX; ++i)
         x_row[i] = (uint32_t)rows_x[min(i * XR + xr, a.slots_x - 1)];
-    // exponents: lane r has up to 16 neighbouring ones of row r, the next stage's first
+    // exponents: lane r has up to 16 neighbouring ones of row r, the next stage's first.  Those after a range's first 16 have 16
+    // at least before them.
     constexpr int SG = STAGE / 32;               // groups of a stage: 2 or 1
     const int groups = (int)(((int64_t)a.N + 31) / 32);
     [[maybe_unused]] const uint8_t *sp = nullptr;
@@ -150,10 +151,13 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     [[maybe_unused]] int have = 0;               // stages that are left in them
     [[maybe_unused]] auto fetch_exps = [&](int s) {
         const int group = s * SG;
-        if (group + 16 <= groups) {
-            __builtin_memcpy(&exps, sp + group, 16);
-        } else {
-            exps = first_of(sp + group, groups - group);
+        __builtin_memcpy(&exps, sp + min(group, groups - 16), 16);
+        // (a row's last ones lie behind others that were there before: 32-bit words, then bytes move down, in place)
+        const int past = group + 16 - groups;
+        if (past > 0) {
+            for (int k = past >> 2; k > 0; --k) exps = uint4v{exps[1], exps[2], exps[3], 0u};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) exps[k] = __builtin_amdgcn_alignbyte(k < 3 ? exps[k < 3 ? k + 1 : 3] : 0u, exps[k], (uint32_t)past & 3u);
         }
         have = 16 / SG;
     };
@@ -167,7 +171,8 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     };
     if constexpr (CKPT) {
         sp = a.S + (int64_t)rows_x[min((int)threadIdx.x, a.slots_x - 1)] * a.lds;
-        fetch_exps(s0);
+        exps = first_of(sp + s0 * SG, groups - s0 * SG);
+        have = 16 / SG;
     }
 
     uint4v hg[PG], hx[PX];
@@ -183,14 +188,18 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     // ---- this wavefront's tiles: places of this lane's pieces of the first half
     const int per = (tiles + kGradWaves - 1) / kGradWaves;
     const int my0 = wave * per, mine = min(per, tiles - my0);
-    uint32_t pa[TILES], pb[TILES], fresh = 0;    // (bit t: tile t's rows of G are not those of tile t - 1)
+    // (units of 16 bytes of G's, of 4 bytes of X's << 16: in registers of their own, sums would be spilled)
+    static_assert(S_AREA <= 4 * 65536, "places of 16 bits");
+    uint32_t places[TILES], fresh = 0, before = 0; // (fresh, bit t: tile t's rows of G are not those of tile t - 1)
     float4v acc[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
         const uint32_t o = t < mine ? a.ops[(int64_t)(first + my0 + t) * 16 + n] : 0u, x = o >> 16;
-        pa[t] = place<GH>(o & 0xffffu, g);
-        pb[t] = X_AREA + (CKPT ? place<XH>(x, g * E / 16) + g * E % 16 : place<XH>(x, g));
-        if (t == 0 || __builtin_amdgcn_readfirstlane(pa[t]) != __builtin_amdgcn_readfirstlane(pa[t > 0 ? t - 1 : 0])) fresh |= 1u << t;
+        const uint32_t pb = X_AREA + (CKPT ? place<XH>(x, g * E / 16) + g * E % 16 : place<XH>(x, g));
+        places[t] = place<GH>(o & 0xffffu, g) / 16 | pb / 4 << 16;
+        const uint32_t window = __builtin_amdgcn_readfirstlane(o & 0xffffu);
+        if (t == 0 || window != before) fresh |= 1u << t;
+        before = window;
         acc[t] = float4v{0.f, 0.f, 0.f, 0.f};
     }
     auto multiply = [&]() {
@@ -198,19 +207,18 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
             if (t >= mine) break;
+            uint32_t at = places[t];
+            asm volatile("" : "+v"(at));         // (or the addresses of all tiles are kept in registers that there are not)
+            const uint32_t pa = (at & 0xffffu) * 16u, pb = at >> 16 << 2;
             if (fresh >> t & 1u) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) x[u] = *reinterpret_cast<const uint4v *>(smem + pa[t] + u * G_HALF);
+                for (int u = 0; u < 2; ++u) x[u] = *reinterpret_cast<const uint4v *>(smem + pa + u * G_HALF);
             }
             uint32_t c[2][CKPT ? E / 4 : 4];
             [[maybe_unused]] uint2v e;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) __builtin_memcpy(c[u], __builtin_assume_aligned(smem + pb[t] + u * X_HALF, CKPT ? E : 16), sizeof c[u]);
-            if constexpr (CKPT) {
-                uint32_t row = pb[t];
-                asm volatile("" : "+v"(row)); // (or the addresses of all tiles are kept in registers that there are not)
-                e = *reinterpret_cast<const uint2v *>(smem + (row / XH * 8u + (S_AREA - X_AREA / XH * 8)));
-            }
+            for (int u = 0; u < 2; ++u) __builtin_memcpy(c[u], __builtin_assume_aligned(smem + pb + u * X_HALF, CKPT ? E : 16), sizeof c[u]);
+            if constexpr (CKPT) e = *reinterpret_cast<const uint2v *>(smem + (pb / XH * 8u + (S_AREA - X_AREA / XH * 8)));
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 uint4v y;
