@@ -38,6 +38,13 @@ struct Rows {
     int64_t g, x; // LDS rows
     int64_t all() const { return g + x; }
 };
+struct Column {
+    int32_t tile, k, slot; // of a tile, with its LDS row
+};
+// The lane that takes LDS row `cls` modulo 16, even ones first; and the row of 16 from LDS row g0 on that a lane takes.
+size_t lane_of(size_t cls) { return cls % 2 * 8 + cls / 2; }
+size_t row_of(size_t lane, int32_t g0) { return (lane % 8 * 2 + lane / 8 + 16 - (size_t)g0 % 16) % 16; }
+
 struct Region {
     int64_t first, n; // run of the tile order
     Rows rows;
@@ -171,6 +178,7 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
     out.inv.resize((size_t)n * 256);
     out.ops.resize((size_t)n * 16);
     std::vector<int32_t> slot_x((size_t)p->K, 0);
+    std::vector<Column> from;
     for (const Region &r : done) {
         out.max_g = std::max(out.max_g, (int)r.rows.g);
         out.max_x = std::max(out.max_x, (int)r.rows.x);
@@ -190,13 +198,26 @@ const GradLayout &get_grad_layout(const ubp_packed *p) {
         for (size_t k = 0; k < x.size(); ++k) slot_x[(size_t)x[k]] = (int32_t)k;
         out.rows.insert(out.rows.end(), x.begin(), x.end());
         out.rows.resize(first_row + (size_t)(out.max_g + out.max_x), out.rows.back());
-        for (int64_t t = 0; t < r.n; ++t) {
-            const Tile &a = tiles[(size_t)o[t]];
-            const int64_t to = r.first + t;
-            const int32_t g0 = (int32_t)(std::lower_bound(g.begin(), g.end(), a.r0) - g.begin());
-            for (int k = 0; k < 16; ++k)
-                out.ops[(size_t)(to * 16 + k)] = (uint32_t)(g0 + k) | (uint32_t)slot_x[(size_t)a.col[k < a.n ? k : 0]] << 16;
-            std::copy(&inv[(size_t)o[t] * 256], &inv[(size_t)o[t] * 256] + 256, &out.inv[(size_t)to * 256]);
+        // The columns of a window's tiles are dealt out anew: LDS rows whose numbers agree modulo 16 lie in the same banks, so
+        // that a tile takes as few of those as it can, and has what it takes in different halves of its lanes.
+        for (int64_t t = 0, after; t < r.n; t = after) {
+            const int32_t r0 = tiles[(size_t)o[t]].r0;
+            from.clear();
+            for (after = t; after < r.n && tiles[(size_t)o[after]].r0 == r0; ++after)
+                for (int k = 0; k < tiles[(size_t)o[after]].n; ++k) from.push_back({o[after], k, slot_x[(size_t)tiles[(size_t)o[after]].col[k]]});
+            std::stable_sort(from.begin(), from.end(), [](const Column &a, const Column &b) { return a.slot % 16 < b.slot % 16; });
+            const int32_t g0 = (int32_t)(std::lower_bound(g.begin(), g.end(), r0) - g.begin());
+            const size_t count = (size_t)(after - t);
+            for (size_t k = 0; k < count * 16; ++k) {
+                const size_t to = (size_t)(r.first + t) + k % count, at = lane_of(k / count);
+                const Column &c = from[k < from.size() ? k : k % count];    // (a place that is left over repeats the tile's first)
+                out.ops[to * 16 + at] = (uint32_t)(g0 + (int32_t)row_of(at, g0)) | (uint32_t)c.slot << 16;
+                for (size_t e = 0; e < 16; ++e) {
+                    const size_t row = row_of(e, g0);
+                    out.inv[to * 256 + (16 * (e >> 2) + at) * 4 + (e & 3)] =
+                        k < from.size() ? inv[(size_t)c.tile * 256 + (16 * (row >> 2) + (size_t)c.k) * 4 + (row & 3)] : -1;
+                }
+            }
         }
         out.regions.insert(out.regions.end(), {(int32_t)r.first, (int32_t)r.n, (int32_t)r.rows.g, (int32_t)r.rows.x});
         out.max_tiles = std::max(out.max_tiles, (int)((r.n + kGradWaves - 1) / kGradWaves));

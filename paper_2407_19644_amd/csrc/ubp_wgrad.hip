@@ -197,9 +197,8 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
         const uint32_t o = t < mine ? a.ops[(int64_t)(first + my0 + t) * 16 + n] : 0u, x = o >> 16;
         const uint32_t pb = X_AREA + (CKPT ? place<XH>(x, g * E / 16) + g * E % 16 : place<XH>(x, g));
         places[t] = place<GH>(o & 0xffffu, g) / 16 | pb / 4 << 16;
-        const uint32_t window = __builtin_amdgcn_readfirstlane(o & 0xffffu);
-        if (t == 0 || window != before) fresh |= 1u << t;
-        before = window;
+        if (t == 0 || __any((o & 0xffffu) != before)) fresh |= 1u << t;
+        before = o & 0xffffu;
         acc[t] = float4v{0.f, 0.f, 0.f, 0.f};
     }
     auto multiply = [&]() {
