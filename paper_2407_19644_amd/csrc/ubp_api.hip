@@ -645,6 +645,9 @@ ubp_status weight_grad(const ubp_packed *p, const void *G, int64_t ldg, const vo
     a.n_tiles = L->n_tiles;
     a.out = dvalues;
     a.accumulate = accumulate ? 1 : 0;
+    // (from the first byte of the first row to the last stage's end in the last)
+    auto far = [](int64_t rows, int64_t pitch) { return pitch > (int64_t(1) << 32) / rows - kGradRowBytes; };
+    a.far_rows = far(p->M, ldg * dtype_size(p->dtype)) || far(p->K, ldx * (saved ? 1 : dtype_size(p->dtype)));
     if (dry) {
         ubp_status rc = launch_weight_grad(a, p->dtype, false, L->shape, stream, true);
         if (rc == UBP_OK) rc = launch_weight_grad(a, p->dtype, true, L->shape, stream, true);

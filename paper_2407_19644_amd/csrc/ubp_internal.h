@@ -408,6 +408,7 @@ struct GradArgs {
     float *out;               // dvalues
     float *part;              // [splits][tiles][256], where splits > 1
     int accumulate;
+    int far_rows;             // G or X reaches over 4 GB
 };
 
 // Gradient of the epilogue.  pass, for kActClamp: what the slope is 1 for.

@@ -18,6 +18,18 @@ template <int BYTES> __device__ __forceinline__ uint32_t place(uint32_t r, uint3
     return r * BYTES + 16u * (BYTES == 64 ? q ^ ((r >> 2) & 3u) : BYTES == 32 ? q ^ ((r >> 3) & 1u) : q);
 }
 
+// LDS by its byte addresses, of which a constant part costs nothing.
+template <typename V> __device__ __forceinline__ V lds_get(uint32_t at, int offset = 0) {
+    typedef __attribute__((address_space(3))) const char *bytes;
+    typedef __attribute__((address_space(3))) const V *values;
+    return *(values)((bytes)(uintptr_t)at + offset);
+}
+template <typename V> __device__ __forceinline__ void lds_put(uint32_t at, V v, int offset = 0) {
+    typedef __attribute__((address_space(3))) char *bytes;
+    typedef __attribute__((address_space(3))) V *values;
+    *(values)((bytes)(uintptr_t)at + offset) = v;
+}
+
 template <typename T> __device__ __forceinline__ float4v product(uint4v a, uint4v b, float4v c);
 template <> __device__ __forceinline__ float4v product<__bf16>(uint4v a, uint4v b, float4v c) {
     return mfma16<true>(__builtin_bit_cast(short8v, a), __builtin_bit_cast(short8v, b), c);
@@ -82,9 +94,12 @@ __device__ __forceinline__ void store_tile(const GradArgs &a, float4v sum, int s
 //    of the SIMD, three of them, cover the way from LDS: operands fetched a tile ahead took registers, and no less time.
 //  * CKPT: X is a checkpoint.  Its codes stay as they are in LDS, and a lane widens its 8 codes of a tile by 4 conversions that
 //    take the exponent along: exact but for fp16 values below its normal range.  Exponents come 16 at a time.
-//  * The last stage of a row may be short; it is staged token by token, zeros behind the last one.
+//  * Rows are 32-bit byte offsets from a place that moves on by a stage: a load takes no arithmetic.  FAR: G or X reaches over
+//    4 GB, and rows are numbers, whose addresses of 64 bits are formed again for every load.
+//  * LDS begins with a checkpoint's exponents, then X, then G, so that the places of both operands of a tile fit one register.
+//  * The last stage of a row may be short; zeros stand behind its last token.
 //  * Ranges of tokens are summed by a second kernel, in order; with one range the sums go straight to their places.
-template <typename T, bool CKPT, int TILES, int GS, int XS>
+template <typename T, bool CKPT, bool FAR, int TILES, int GS, int XS>
 __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     constexpr int E = 16 / (int)sizeof(T);       // tokens of a 16-byte piece
     constexpr int STAGE = 8 * E;                 // tokens of a stage
@@ -92,13 +107,12 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     constexpr int GH = kRowBytes / 2, XH = XB / 2; // of half a stage
     // Halves lie 64 bytes more apart than their rows take: the 8 lanes that LDS serves together write one row's pieces of both
     // halves (or two or four rows of codes), which would meet in the same banks.
-    constexpr int G_HALF = GS * GH + 64, X_HALF = XS * XH + 64, X_AREA = 2 * G_HALF, S_AREA = X_AREA + 2 * X_HALF;
+    constexpr int G_HALF = GS * GH + 64, X_HALF = XS * XH + 64, X_AREA = CKPT ? 8 * XS : 0, G_AREA = X_AREA + 2 * X_HALF;
     constexpr int XL = XB / 16;                  // lanes that load it
     constexpr int GR = kThreads / 8, XR = kThreads / XL; // rows at once
     constexpr int PG = (GS + GR - 1) / GR, PX = (XS + XR - 1) / XR; // loads per lane
     static_assert(XS <= kThreads, "a lane per row for the exponents");
-    static_assert(X_AREA % XH == 0, "an exponent's place follows from its row's");
-    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    static_assert((G_AREA + G_HALF) / 2 <= 65536 && X_HALF <= 65536 && G_AREA % 16 == 0, "places of 16 bits");
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     const uint32_t g = (uint32_t)(lane >> 4), n = (uint32_t)(lane & 15);
@@ -119,29 +133,32 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     const int s0 = split * a.per_split, s1 = split == a.splits - 1 ? all : s0 + a.per_split, f1 = min(s1, full);
 
     // this lane's rows: pass i takes row list entries i GR + thread / 8 (of X: i XR + thread / XL), at a place a constant further on
-    uint32_t g_row[PG], x_row[PX];               // (their numbers: addresses of 64 bits for all of them would be spilled)
+    uint32_t g_row[PG], x_row[PX];
     const uint32_t gq = threadIdx.x % 8, xq = threadIdx.x % XL;
     const int gr = (int)threadIdx.x / 8, xr = (int)threadIdx.x / XL;
     const int64_t g_pitch = a.ldg * (int)sizeof(T), x_pitch = a.ldx * (CKPT ? 1 : (int)sizeof(T));
     const char *gbase = static_cast<const char *>(a.G) + (int64_t)s0 * kRowBytes, *xbase = static_cast<const char *>(a.X) + (int64_t)s0 * XB;
-    auto g_piece = [&](int i) {
-        asm volatile("" : "+v"(g_row[i]));
-        return gbase + ((int64_t)g_row[i] * g_pitch + 16 * gq);
+    auto piece = [&](uint32_t &row, const char *base, int64_t pitch, uint32_t q) {
+        asm volatile("" : "+v"(row));            // (or all addresses are kept, in registers that there are not)
+        if constexpr (FAR) return base + ((int64_t)row * pitch + 16 * q);
+        else return base + row;
     };
-    auto x_piece = [&](int i) {
-        asm volatile("" : "+v"(x_row[i]));
-        return xbase + ((int64_t)x_row[i] * x_pitch + 16 * xq);
-    };
-    auto g_place = [&](uint32_t slot, uint32_t q) { return q / 4 * G_HALF + place<GH>(slot, q % 4); };
+    auto g_piece = [&](int i) { return piece(g_row[i], gbase, g_pitch, gq); };
+    auto x_piece = [&](int i) { return piece(x_row[i], xbase, x_pitch, xq); };
+    auto g_place = [&](uint32_t slot, uint32_t q) { return G_AREA + q / 4 * G_HALF + place<GH>(slot, q % 4); };
     auto x_place = [&](uint32_t slot, uint32_t q) { return X_AREA + q / (XL / 2) * X_HALF + place<XH>(slot, q % (XL / 2)); };
     const uint32_t gu = g_place((uint32_t)gr, gq), xu = x_place((uint32_t)xr, xq);
     static_assert(GR % 16 == 0 && XR % 16 == 0, "the rows of two passes differ by a multiple of 16: their places by a constant");
 #pragma unroll
-    for (int i = 0; i < PG; ++i)
+    for (int i = 0; i < PG; ++i) {
         g_row[i] = (uint32_t)rows_g[min(i * GR + gr, a.slots_g - 1)];
+        if (!FAR) g_row[i] = g_row[i] * (uint32_t)g_pitch + 16 * gq;
+    }
 #pragma unroll
-    for (int i = 0; i < PX; ++i)
+    for (int i = 0; i < PX; ++i) {
         x_row[i] = (uint32_t)rows_x[min(i * XR + xr, a.slots_x - 1)];
+        if (!FAR) x_row[i] = x_row[i] * (uint32_t)x_pitch + 16 * xq;
+    }
     // exponents: lane r has up to 16 neighbouring ones of row r, the next stage's first.  Those after a range's first 16 have 16
     // at least before them.
     constexpr int SG = STAGE / 32;               // groups of a stage: 2 or 1
@@ -164,7 +181,7 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     // a stage's exponents as the floats that conversions take, two for each row
     [[maybe_unused]] auto put_exps = [&]() {
         const uint32_t b0 = exps[0] & 0xffu, b1 = SG == 2 ? (exps[0] >> 8) & 0xffu : b0;
-        if ((int)threadIdx.x < x_slots) *reinterpret_cast<uint2v *>(smem + S_AREA + 8 * threadIdx.x) = uint2v{b0 << 23, b1 << 23};
+        if ((int)threadIdx.x < x_slots) lds_put(8 * threadIdx.x, uint2v{b0 << 23, b1 << 23});
 #pragma unroll
         for (int k = 0; k < 4; ++k) exps[k] = exps[k] >> (8 * SG) | (k < 3 ? exps[k < 3 ? k + 1 : 3] << (32 - 8 * SG) : 0u);
         --have;
@@ -188,15 +205,14 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     // ---- this wavefront's tiles: places of this lane's pieces of the first half
     const int per = (tiles + kGradWaves - 1) / kGradWaves;
     const int my0 = wave * per, mine = min(per, tiles - my0);
-    // (units of 16 bytes of G's, of 4 bytes of X's << 16: in registers of their own, sums would be spilled)
-    static_assert(S_AREA <= 4 * 65536, "places of 16 bits");
+    // (half of G's, X's behind X_AREA << 16)
     uint32_t places[TILES], fresh = 0, before = 0; // (fresh, bit t: tile t's rows of G are not those of tile t - 1)
     float4v acc[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
         const uint32_t o = t < mine ? a.ops[(int64_t)(first + my0 + t) * 16 + n] : 0u, x = o >> 16;
-        const uint32_t pb = X_AREA + (CKPT ? place<XH>(x, g * E / 16) + g * E % 16 : place<XH>(x, g));
-        places[t] = place<GH>(o & 0xffffu, g) / 16 | pb / 4 << 16;
+        const uint32_t pb = CKPT ? place<XH>(x, g * E / 16) + g * E % 16 : place<XH>(x, g);
+        places[t] = (G_AREA + place<GH>(o & 0xffffu, g)) / 2 | pb << 16;
         if (t == 0 || __any((o & 0xffffu) != before)) fresh |= 1u << t;
         before = o & 0xffffu;
         acc[t] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -208,25 +224,28 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
             if (t >= mine) break;
             uint32_t at = places[t];
             asm volatile("" : "+v"(at));         // (or the addresses of all tiles are kept in registers that there are not)
-            const uint32_t pa = (at & 0xffffu) * 16u, pb = at >> 16 << 2;
+            const uint32_t pa = (at & 0xffffu) * 2u, pb = at >> 16;
             if (fresh >> t & 1u) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) x[u] = *reinterpret_cast<const uint4v *>(smem + pa + u * G_HALF);
+                for (int u = 0; u < 2; ++u) x[u] = lds_get<uint4v>(pa, u * G_HALF);
             }
-            uint32_t c[2][CKPT ? E / 4 : 4];
+            typedef __attribute__((__vector_size__(CKPT ? E : 16))) uint32_t piece_t;
+            piece_t c[2];
             [[maybe_unused]] uint2v e;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) __builtin_memcpy(c[u], __builtin_assume_aligned(smem + pb + u * X_HALF, CKPT ? E : 16), sizeof c[u]);
-            if constexpr (CKPT) e = *reinterpret_cast<const uint2v *>(smem + (pb / XH * 8u + (S_AREA - X_AREA / XH * 8)));
+            for (int u = 0; u < 2; ++u) c[u] = lds_get<piece_t>(pb, X_AREA + u * X_HALF);
+            if constexpr (CKPT) e = lds_get<uint2v>(pb / XH * 8u);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 uint4v y;
                 if constexpr (CKPT) {
                     T w[E];
-                    e4m3_to<T, E>(c[u], __builtin_bit_cast(float, (uint32_t)e[u]), w);
+                    uint32_t codes[E / 4];
+                    __builtin_memcpy(codes, &c[u], sizeof codes);
+                    e4m3_to<T, E>(codes, __builtin_bit_cast(float, (uint32_t)e[u]), w);
                     __builtin_memcpy(&y, w, 16);
                 } else {
-                    __builtin_memcpy(&y, c[u], 16);
+                    __builtin_memcpy(&y, &c[u], 16);
                 }
                 acc[t] = product<T>(x[u], y, acc[t]);
             }
@@ -245,13 +264,13 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
 #pragma unroll
         for (int i = 0; i < PG; ++i) {
             if (i * GR >= g_slots) continue;
-            if (i * GR + gr < g_slots) *reinterpret_cast<uint4v *>(smem + gu + i * (GR * GH)) = hg[i];
+            if (i * GR + gr < g_slots) lds_put(gu, hg[i], i * (GR * GH));
             if (more) __builtin_memcpy(&hg[i], g_piece(i), 16);
         }
 #pragma unroll
         for (int i = 0; i < PX; ++i) {
             if (i * XR >= x_slots) continue;
-            if (i * XR + xr < x_slots) *reinterpret_cast<uint4v *>(smem + xu + i * (XR * XH)) = hx[i];
+            if (i * XR + xr < x_slots) lds_put(xu, hx[i], i * (XR * XH));
             if (more) __builtin_memcpy(&hx[i], x_piece(i), 16);
         }
         lds_barrier();
@@ -267,14 +286,14 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
             const bool in_g = slot < g_slots;
             const T *src = in_g ? static_cast<const T *>(a.G) + (int64_t)rows_g[slot] * a.ldg : static_cast<const T *>(a.X) + (int64_t)rows_x[slot - g_slots] * a.ldx;
             const uint4v o = first_of(src + n0 + q * E, a.N - n0 - q * E);
-            *reinterpret_cast<uint4v *>(smem + (in_g ? g_place((uint32_t)slot, (uint32_t)q) : x_place((uint32_t)(slot - g_slots), (uint32_t)q))) = o;
+            lds_put(in_g ? g_place((uint32_t)slot, (uint32_t)q) : x_place((uint32_t)(slot - g_slots), (uint32_t)q), o);
         }
         if constexpr (CKPT)
             for (int p = threadIdx.x; p < x_slots * XL; p += kThreads) {
                 const int slot = p / XL, q = p % XL, col = n0 + q * 16;
                 const uint8_t *src = static_cast<const uint8_t *>(a.X) + (int64_t)rows_x[slot] * a.ldx;
                 const uint4v codes = first_of(src + col, a.N - col);
-                *reinterpret_cast<uint4v *>(smem + x_place((uint32_t)slot, (uint32_t)q)) = codes;
+                lds_put(x_place((uint32_t)slot, (uint32_t)q), codes);
             }
         __syncthreads();
         multiply();
@@ -307,12 +326,12 @@ __global__ __launch_bounds__(256) void weight_sum_kernel(GradArgs a) {
         if ((int32_t)to[e] >= 0) a.out[to[e]] = a.accumulate ? a.out[to[e]] + sum[e] : sum[e];
 }
 
-template <typename T, bool CKPT, int SHAPE> ubp_status launch_one(GradArgs a, hipStream_t st, bool dry) {
+template <typename T, bool CKPT, bool FAR, int SHAPE> ubp_status launch_one(GradArgs a, hipStream_t st, bool dry) {
     constexpr GradShape S = kGradShapes[SHAPE];
-    constexpr auto kernel = &weight_grad_kernel<T, CKPT, S.tiles, S.g_slots, S.x_slots>;
+    constexpr auto kernel = &weight_grad_kernel<T, CKPT, FAR, S.tiles, S.g_slots, S.x_slots>;
     constexpr int STAGE = kRowBytes / (int)sizeof(T);
     static LdsLimit limit;
-    const ubp_status rc = limit.raise(reinterpret_cast<const void *>(kernel));
+    const ubp_status rc = limit.raise(reinterpret_cast<const void *>(kernel), true);
     if (rc != UBP_OK || dry) return rc;
     const int64_t grid = 8 * (((int64_t)a.n_regions * a.splits + 7) / 8);
     if (grid * kThreads >= (int64_t(1) << 32)) return UBP_ERR_UNSUPPORTED; // (a launch's threads are counted in 32 bits)
@@ -323,12 +342,19 @@ template <typename T, bool CKPT, int SHAPE> ubp_status launch_one(GradArgs a, hi
     return launch_kernel(kernel, dim3((unsigned)grid), dim3(kThreads), lds, st, a);
 }
 
+template <typename T, bool CKPT, int SHAPE> ubp_status launch_shape(const GradArgs &a, hipStream_t st, bool dry) {
+    if (dry) {
+        const ubp_status rc = launch_one<T, CKPT, false, SHAPE>(a, st, dry);
+        return rc != UBP_OK ? rc : launch_one<T, CKPT, true, SHAPE>(a, st, dry);
+    }
+    return a.far_rows ? launch_one<T, CKPT, true, SHAPE>(a, st, dry) : launch_one<T, CKPT, false, SHAPE>(a, st, dry);
+}
 template <typename T, bool CKPT> ubp_status launch_t(const GradArgs &a, int shape, hipStream_t st, bool dry) {
     static_assert(kNumGradShapes == 3, "their instantiations");
     switch (shape) {
-    case 0: return launch_one<T, CKPT, 0>(a, st, dry);
-    case 1: return launch_one<T, CKPT, 1>(a, st, dry);
-    case 2: return launch_one<T, CKPT, 2>(a, st, dry);
+    case 0: return launch_shape<T, CKPT, 0>(a, st, dry);
+    case 1: return launch_shape<T, CKPT, 1>(a, st, dry);
+    case 2: return launch_shape<T, CKPT, 2>(a, st, dry);
     }
     return UBP_ERR_UNSUPPORTED;
 }
