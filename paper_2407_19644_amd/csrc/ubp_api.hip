@@ -530,12 +530,9 @@ ubp_status execute(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t 
 // Tokens of a call, at most: the kernels count columns, and run a workgroup's columns past the last one, in 32 bits.
 constexpr int32_t kMaxTokens = 0x7fffffff - 0xffff;
 
-// Workgroups of a row of the epilogue's gradient: one per row where the rows fill the card by themselves, else one per 4 chunks
-// (sums of parts then meet in a second launch).
-int act_row_groups(int M, int N) {
-    const int chunks = (int)(((int64_t)N + kActChunk - 1) / kActChunk);
-    return M >= 1024 || chunks <= 4 ? 1 : (chunks + 3) / 4;
-}
+// Workgroups of a row of the epilogue's gradient: one where the rows fill the card by themselves, else one per kActGroup tokens
+// (sums of groups then meet in a second launch).
+int act_row_groups(int M, int N) { return M >= 1024 ? 1 : std::max(1, (int)(((int64_t)N + kActGroup - 1) / kActGroup)); }
 
 ubp_status linear_grad(const ubp_packed *p, const void *dY, int64_t lddy, const void *Z, int64_t ldz, int32_t N, void *G, int64_t ldg,
                        float *dbias, int32_t activation, float lo, float hi, void *workspace, int64_t workspace_bytes, void *stream) {
@@ -563,7 +560,6 @@ ubp_status linear_grad(const ubp_packed *p, const void *dY, int64_t lddy, const 
     a.hi = activation == UBP_ACT_CLAMP ? hi : INFINITY;
     a.dbias = dbias;
     a.row_groups = act_row_groups(p->M, N);
-    a.group_chunks = a.row_groups > 1 ? 4 : std::max(1, (int)(((int64_t)N + kActChunk - 1) / kActChunk));
     if (dbias && a.row_groups > 1) {
         if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0 || workspace_bytes < (int64_t)p->M * a.row_groups * 4)
             return UBP_ERR_INVALID_ARG;

@@ -420,9 +420,9 @@ struct ActGradArgs {
     int M, N, act, pass;
     float c1, c3, lo, hi;
     float *dbias, *part;      // part: [M][row_groups], where row_groups > 1
-    int row_groups, group_chunks; // workgroups of a long row, chunks of kActChunk tokens of each
+    int row_groups;           // workgroups of a row, kActGroup tokens each where they are several
 };
-constexpr int kActChunk = 2048;
+constexpr int kActGroup = 8192;
 
 // A checkpoint: X -> Q, S, or Q, S -> out (pitch ldx).
 struct CheckpointArgs {

@@ -29,65 +29,58 @@ __device__ __forceinline__ float slope(const ActGradArgs &a, float z) {
     return z == z ? r : z;
 }
 
-// A wavefront takes kActChunk neighbouring tokens of a row, all its loads issued first: G = dY act'(Z), and the sum of G's
-// fp32 values, before they are rounded.  Four wavefronts of a workgroup take a row each, or, where rows are longer than a
-// chunk, chunks of one row, whose sums meet in LDS in order.
-// What bounds it: memory.  4096 rows of 8192 bf16 tokens, SiLU: 51 us, 3.96 TB/s (a large copy: 4.92); 960 rows of 1568 fp16
-// tokens, GELU: 7.9 us, as long as the launch and one wavefront's way through its row.
+// A lane takes 16 bytes of neighbouring tokens of a row at once, a wavefront a part of 1 KB: G = dY act'(Z), and the sum of
+// G's fp32 values, before they are rounded.  Four wavefronts of a workgroup take a row each, or, where rows are longer than a
+// part, every fourth part of one row (of kActGroup tokens of it, where rows are few), whose sums meet in LDS in order.
+// What bounds it: memory.  4096 rows of 8192 bf16 tokens, SiLU: 44 us, 4.58 TB/s (a large copy: 4.92).  One load of each matrix
+// in flight per lane leaves room for 8 wavefronts per SIMD; four, with 5 wavefronts, took 54 us.  960 rows of 1568 fp16 tokens:
+// 7.9 us, the launch.
 template <typename T>
 __global__ __launch_bounds__(256) void act_grad_kernel(ActGradArgs a) {
-    constexpr int E = 16 / (int)sizeof(T), CHUNK = kActChunk, U = CHUNK / (64 * E);
+    constexpr int E = 16 / (int)sizeof(T), PART = 64 * E;
+    static_assert(kActGroup % (4 * PART) == 0, "a group is whole rounds of parts");
     __shared__ float sums[4];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
-    const int chunks = (a.N + CHUNK - 1) / CHUNK;
-    const bool shared = chunks > 1;
+    const bool shared = a.N > PART;
     const int64_t unit = (int64_t)blockIdx.x;
     const int64_t row = shared ? unit / a.row_groups : 4 * unit + wave;
-    const int part = shared ? (int)(unit % a.row_groups) : 0;
+    const int group = shared ? (int)(unit % a.row_groups) : 0;
     if (row >= a.M) return;                     // (whole workgroups where rows are shared)
     const T *dy = static_cast<const T *>(a.dY) + row * a.lddy, *z = static_cast<const T *>(a.Z) + row * a.ldz;
     T *gout = static_cast<T *>(a.G) + row * a.ldg;
     float sum = 0.f;
-    for (int c = part * a.group_chunks + (shared ? wave : 0), end = min((part + 1) * a.group_chunks, chunks); c < end; c += 4) {
-        const int n0 = c * CHUNK + lane * E;
-        T y[U][E], zz[U][E];
+    const int first = group * kActGroup, last = a.row_groups > 1 ? min(first + kActGroup, a.N) : a.N;
+    for (int n0 = first + (shared ? wave * PART : 0); n0 < last; n0 += 4 * PART) {
+        const int col = n0 + lane * E;
+        T y[E], zz[E], o[E];
+        if (col + E <= a.N) {
+            __builtin_memcpy(y, dy + col, 16);
+            if (a.pass != kPassAll) __builtin_memcpy(zz, z + col, 16);
+        } else {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int col = n0 + u * 64 * E;
-            if (col + E <= a.N) {
-                __builtin_memcpy(y[u], dy + col, 16);
-                if (a.pass != kPassAll) __builtin_memcpy(zz[u], z + col, 16);
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    y[u][e] = zz[u][e] = (T)0.f;
-                    if (col + e < a.N) {
-                        y[u][e] = dy[col + e];
-                        if (a.pass != kPassAll) zz[u][e] = z[col + e];
-                    }
+            for (int e = 0; e < E; ++e) {
+                y[e] = zz[e] = (T)0.f;
+                if (col + e < a.N) {
+                    y[e] = dy[col + e];
+                    if (a.pass != kPassAll) zz[e] = z[col + e];
                 }
             }
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int col = n0 + u * 64 * E;
-            T o[E];
+        for (int e = 0; e < E; ++e) {
+            // (a slope of 0 of ReLU and clamp stops what comes, whatever it is)
+            const float s = slope(a, to_f32(zz[e])), d = to_f32(y[e]);
+            const float v = a.act == kActClamp ? (s != 0.f ? d : 0.f) : d * s;
+            sum += v;
+            o[e] = from_f32<T>(v);
+        }
+        if (col + E <= a.N) {
+            __builtin_memcpy(gout + col, o, 16);
+        } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                // (a slope of 0 of ReLU and clamp stops what comes, whatever it is)
-                const float s = slope(a, to_f32(zz[u][e])), d = to_f32(y[u][e]);
-                const float v = a.act == kActClamp ? (s != 0.f ? d : 0.f) : d * s;
-                sum += v;
-                o[e] = from_f32<T>(v);
-            }
-            if (col + E <= a.N) {
-                __builtin_memcpy(gout + col, o, 16);
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (col + e < a.N) gout[col + e] = o[e];
-            }
+            for (int e = 0; e < E; ++e)
+                if (col + e < a.N) gout[col + e] = o[e];
         }
     }
     if (a.dbias == nullptr) return;
@@ -102,7 +95,7 @@ __global__ __launch_bounds__(256) void act_grad_kernel(ActGradArgs a) {
     if (threadIdx.x == 0) {
         const float s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
         if (a.row_groups == 1) a.dbias[row] = s;
-        else a.part[row * a.row_groups + part] = s;
+        else a.part[row * a.row_groups + group] = s;
     }
 }
 
@@ -116,11 +109,11 @@ __global__ __launch_bounds__(256) void row_sum_kernel(ActGradArgs a) {
 }
 
 template <typename T> ubp_status act_grad(ActGradArgs a, hipStream_t st) {
-    const int chunks = (a.N + kActChunk - 1) / kActChunk;
-    const int64_t grid = chunks > 1 ? (int64_t)a.M * a.row_groups : ((int64_t)a.M + 3) / 4;
+    const bool shared = a.N > 64 * 16 / (int)sizeof(T);
+    const int64_t grid = shared ? (int64_t)a.M * a.row_groups : ((int64_t)a.M + 3) / 4;
     if (grid * 256 >= (int64_t(1) << 32)) return UBP_ERR_UNSUPPORTED; // (a launch's threads are counted in 32 bits)
     const ubp_status rc = launch_kernel(&act_grad_kernel<T>, dim3((unsigned)grid), dim3(256), 0, st, a);
-    if (rc != UBP_OK || a.dbias == nullptr || chunks <= 1 || a.row_groups == 1) return rc;
+    if (rc != UBP_OK || a.dbias == nullptr || a.row_groups == 1) return rc;
     return launch_kernel(&row_sum_kernel, dim3((unsigned)((a.M + 255) / 256)), dim3(256), 0, st, a);
 }
 
