@@ -99,8 +99,8 @@ __device__ __forceinline__ void store_tile(const GradArgs &a, float4v sum, int s
 //  * LDS begins with a checkpoint's exponents, then X, then G, so that the places of both operands of a tile fit one register.
 //  * The last stage of a row may be short; zeros stand behind its last token.
 //  * Ranges of tokens are summed by a second kernel, in order; with one range the sums go straight to their places.
-// Measured: 4096 x 4096, 10 % in 16 x 16 blocks, bf16, 8192 tokens from a checkpoint: 110 us with the second kernel's 9 (inputs in
-// rotation), 250 TFLOP/s of kept products; 256 x 2304, 25 % in 4 x 4 blocks, 12544 tokens: 39 us.  What bounds it: the stages'
+// Measured: 4096 x 4096, 10 % in 16 x 16 blocks, bf16, 8192 tokens from a checkpoint: 107 us with the second kernel's 9 (inputs in
+// rotation), 256 TFLOP/s of kept products; 256 x 2304, 25 % in 4 x 4 blocks, 12544 tokens: 38 us.  What bounds it: the stages'
 // parts, one behind the other.  Of the first: 11 us before and after the stages, 27 for the way into LDS and its barriers, 42 for
 // the products (LDS has 28 % of its cycles taken), 12 in which loads are waited for; loads by themselves take 40.  Two stages in
 // LDS, which would overlap them, leave room for half the rows: regions are smaller and read rows more often (143 us, and 41).
@@ -208,8 +208,9 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
     }
 
     // ---- this wavefront's tiles: places of this lane's pieces of the first half
-    const int per = (tiles + kGradWaves - 1) / kGradWaves;
-    const int my0 = wave * per, mine = min(per, tiles - my0);
+    // (what is left over goes to the first wavefronts, one to each SIMD in turn)
+    const int per = tiles / kGradWaves, more_of = tiles % kGradWaves;
+    const int my0 = wave * per + min(wave, more_of), mine = per + (wave < more_of ? 1 : 0);
     // (half of G's, X's behind X_AREA << 16)
     uint32_t places[TILES], fresh = 0, before = 0; // (fresh, bit t: tile t's rows of G are not those of tile t - 1)
     float4v acc[TILES];
