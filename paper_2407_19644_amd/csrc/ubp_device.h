@@ -108,7 +108,7 @@ constexpr bool kWide = false;
 // Epilogue with on == 2, without the residual.
 __device__ __forceinline__ void epilogue_act(const Epilogue &e, float *v, int n, float b) {
     if (e.act == kActSigmoid && e.c3 == 0.f) {
-        // (SiLU: no powers that could overflow.  5 instructions fewer: 4096 x 4096 with 8192 pixels and a residual takes 106 us, not 109)
+        // (SiLU: no powers that could overflow.  5 instructions fewer: kernel 6 on 4096 x 4096 with 8192 pixels took 103 us, not 109)
 #pragma unroll
         for (int i = 0; i < n; ++i) {
             const float x = v[i] + b;
