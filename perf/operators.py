@@ -27,29 +27,29 @@ def _case(name, op, M, K, N, dtype, block=(4, 4), density=0.25, act="none", bias
 def listed():
     return [
         # one token through a pruned projection: what serving does for every layer and token; latency
-        _case("linear 1 token 4096x4096", "linear", 4096, 4096, 1, "bf16", (16, 16), 0.10, "silu", True, True),
+        _case("linear, 1 token, 4096 x 4096", "linear", 4096, 4096, 1, "bf16", (16, 16), 0.10, "silu", True, True),
         # a small layer with small blocks and an ordinary number of tokens
-        _case("linear 1568 tokens 960x160", "linear", 960, 160, 1568, "f16", (4, 4), 0.30, "gelu", True, True),
+        _case("linear, 1568 tokens, 960 x 160", "linear", 960, 160, 1568, "f16", (4, 4), 0.30, "gelu", True, True),
         # the largest layer, a batch of training or prefill
-        _case("linear 8192 tokens 4096x4096", "linear", 4096, 4096, 8192, "bf16", (16, 16), 0.10, "silu", True, True),
+        _case("linear, 8192 tokens, 4096 x 4096", "linear", 4096, 4096, 8192, "bf16", (16, 16), 0.10, "silu", True, True),
         # backward of the small layer's epilogue
-        _case("linear_grad 1568 tokens 960 rows", "linear_grad", 960, 160, 1568, "f16", (4, 4), 0.30, "gelu", True),
+        _case("linear_grad, 1568 tokens, 960 rows", "linear_grad", 960, 160, 1568, "f16", (4, 4), 0.30, "gelu", True),
         # backward of the largest layer's epilogue
-        _case("linear_grad 8192 tokens 4096 rows", "linear_grad", 4096, 4096, 8192, "bf16", (16, 16), 0.10, "silu", True),
+        _case("linear_grad, 8192 tokens, 4096 rows", "linear_grad", 4096, 4096, 8192, "bf16", (16, 16), 0.10, "silu", True),
         # inputs of the small layer, kept in 8 bits
-        _case("checkpoint 1568 tokens 160 rows", "checkpoint", 960, 160, 1568, "f16", (4, 4), 0.30),
+        _case("checkpoint, 1568 tokens, 160 rows", "checkpoint", 960, 160, 1568, "f16", (4, 4), 0.30),
         # a ragged number of tokens: rows start at any alignment, the last group is short
-        _case("checkpoint 12543 tokens 2304 rows", "checkpoint", 256, 2304, 12543, "bf16", (4, 4), 0.25),
+        _case("checkpoint, 12543 tokens, 2304 rows", "checkpoint", 256, 2304, 12543, "bf16", (4, 4), 0.25),
         # inputs of the largest layer
-        _case("checkpoint 8192 tokens 4096 rows", "checkpoint", 4096, 4096, 8192, "bf16", (16, 16), 0.10),
+        _case("checkpoint, 8192 tokens, 4096 rows", "checkpoint", 4096, 4096, 8192, "bf16", (16, 16), 0.10),
         # fp32 training of a tiny layer; latency
-        _case("weight_grad 196 tokens 64x64", "weight_grad", 64, 64, 196, "f32", (4, 4), 0.50),
+        _case("weight_grad, 196 tokens, 64 x 64", "weight_grad", 64, 64, 196, "f32", (4, 4), 0.50),
         # small layer, ragged number of tokens, inputs as they were
-        _case("weight_grad 1567 tokens 960x160", "weight_grad", 960, 160, 1567, "f16", (4, 4), 0.30),
+        _case("weight_grad, 1567 tokens, 960 x 160", "weight_grad", 960, 160, 1567, "f16", (4, 4), 0.30),
         # small blocks, many tokens, inputs from the checkpoint
-        _case("weight_grad 12544 tokens 256x2304", "weight_grad", 256, 2304, 12544, "bf16", (4, 4), 0.25, ckpt=True),
+        _case("weight_grad, 12544 tokens, 256 x 2304", "weight_grad", 256, 2304, 12544, "bf16", (4, 4), 0.25, ckpt=True),
         # the largest layer, inputs from the checkpoint
-        _case("weight_grad 8192 tokens 4096x4096", "weight_grad", 4096, 4096, 8192, "bf16", (16, 16), 0.10, ckpt=True),
+        _case("weight_grad, 8192 tokens, 4096 x 4096", "weight_grad", 4096, 4096, 8192, "bf16", (16, 16), 0.10, ckpt=True),
     ]
 
 
