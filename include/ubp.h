@@ -214,8 +214,8 @@ ubp_status ubp_spmm_plan(const ubp_packed *p, const void *X_dev, int64_t ldx, in
  * to y_dtype.  All kernels support it; nothing else about the call changes.
  *   bias_dev   : DEVICE pointer to M floats (one per output channel / row of Y), or NULL (no bias).
  *   activation : 0 none; 1 ReLU, max(v, 0); 2 clamp to [lo, hi] (requires lo <= hi, else
- *                UBP_ERR_INVALID_ARG).  max / min are IEEE maxNum / minNum: a NaN becomes the
- *                lower bound.  lo / hi are ignored for 0 and 1.
+ *                UBP_ERR_INVALID_ARG).  max / min are IEEE maxNum / minNum: with 1 and 2 a NaN
+ *                becomes the lower bound; with 0 it stays one.  lo / hi are ignored for 0 and 1.
  * epilogue == NULL, or no bias and activation 0, is ubp_spmm / ubp_spmm_plan; plan may be NULL.
  */
 typedef struct {
@@ -245,7 +245,7 @@ enum {
  * X - is as for ubp_spmm_fused; ubp_spmm_prepare with the same arguments prepares it.
  *   bias_dev     : as in ubp_epilogue.
  *   activation   : UBP_ACT_*; UBP_ACT_CLAMP requires lo <= hi.  ReLU and clamp turn a NaN into the lower bound; with the
- *                  others a NaN stays one, and v = -Inf gives NaN.
+ *                  others a NaN stays one.  v = -Inf gives NaN with the last three (-Inf times a distribution function of 0).
  *   residual_dev : DEVICE pointer to an M x N matrix of y_dtype, leading dimension ldr (elements, >= N; any alignment), or
  *                  NULL.  It must not share memory with Y, which is checked (UBP_ERR_INVALID_ARG): a layer adds to a
  *                  residual stream by writing the next one.  It may lie beside Y in rows of one pitch.

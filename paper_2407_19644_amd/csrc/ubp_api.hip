@@ -300,8 +300,9 @@ ubp_status epilogue_of(const ubp_linear_epilogue *fused, Epilogue &ep) {
     ep.res = fused->residual_dev;
     ep.ldr = fused->ldr;
     ep.on = (ep.res != nullptr || act > UBP_ACT_CLAMP) ? 2 : (ep.bias != nullptr || act != UBP_ACT_NONE) ? 1 : 0;
-    ep.lo = act == UBP_ACT_RELU ? 0.f : act == UBP_ACT_CLAMP ? fused->lo : -INFINITY;
-    ep.hi = act == UBP_ACT_CLAMP ? fused->hi : INFINITY;
+    // (maxNum and minNum leave a value alone where the bound is NaN, a NaN among them)
+    ep.lo = act == UBP_ACT_RELU ? 0.f : act == UBP_ACT_CLAMP ? fused->lo : NAN;
+    ep.hi = act == UBP_ACT_RELU ? INFINITY : act == UBP_ACT_CLAMP ? fused->hi : NAN;
     activation_of(act, ep.act, ep.c1, ep.c3);
     return UBP_OK;
 }

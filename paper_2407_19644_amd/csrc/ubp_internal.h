@@ -290,8 +290,8 @@ struct TileLayoutDev {
 // ------------------------------------------------------------------ kernel arguments
 // What happens to an output value between the accumulator and the store: Y = act(acc + bias[row]) + res[row][pixel],
 // in fp32, before the one rounding to Y's type.  on == 0: nothing.  on == 1: no residual, and the activation is a clamp to
-// [lo, hi] (ReLU: lo = 0, hi = +inf), taken with maxNum / minNum, so that a NaN becomes lo.  on == 2: the activation is
-// `act`, and res, where there is one, is added.
+// [lo, hi] (ReLU: lo = 0, hi = +inf), taken with maxNum / minNum, so that a NaN becomes lo; no activation: both bounds are NaN,
+// which leaves every value alone.  on == 2: the activation is `act`, and res, where there is one, is added.
 enum : int { kActClamp = 0, kActSigmoid = 1, kActNormal = 2 };
 struct Epilogue {
     const float *bias; // device, M floats, or null
