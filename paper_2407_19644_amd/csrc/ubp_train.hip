@@ -29,9 +29,26 @@ __device__ __forceinline__ float slope(const ActGradArgs &a, float z) {
     return z == z ? r : z;
 }
 
+// A sum of any length, to about 2^-24 of the sum of magnitudes: what an addition drops is kept beside it (one addition after the
+// other would be off by up to n 2^-25 of itself where terms are of one size; a row may have millions).
+struct LongSum {
+    float sum = 0.f, low = 0.f;
+    __device__ __forceinline__ void add(float v) {
+        const float s = sum + v, t = s - sum;
+        low += (sum - (s - t)) + (v - t);
+        sum = s;
+    }
+    // (beside an Inf or NaN stands nothing that counts)
+    __device__ __forceinline__ float value() const {
+        const float s = sum + low;
+        return fabsf(s) < INFINITY ? s : sum;
+    }
+};
+
 // A lane takes 16 bytes of neighbouring tokens of a row at once, a wavefront a part of 1 KB: G = dY act'(Z), and the sum of
 // G's fp32 values, before they are rounded.  Four wavefronts of a workgroup take a row each, or, where rows are longer than a
-// part, every fourth part of one row (of kActGroup tokens of it, where rows are few), whose sums meet in LDS in order.
+// part, every fourth part of one row (of kActGroup tokens of it, where rows are few), whose sums meet in LDS in order.  A lane's
+// sums of its 16 bytes are added up by LongSum, however many they are.
 // What bounds it: memory.  4096 rows of 8192 bf16 tokens, SiLU: 44 us, 4.58 TB/s (a large copy: 4.92).  One load of each matrix
 // in flight per lane leaves room for 8 wavefronts per SIMD; four, with 5 wavefronts, took 54 us.  960 rows of 1568 fp16 tokens:
 // 7.9 us, the launch.
@@ -49,7 +66,7 @@ __global__ __launch_bounds__(256) void act_grad_kernel(ActGradArgs a) {
     if (row >= a.M) return;                     // (whole workgroups where rows are shared)
     const T *dy = static_cast<const T *>(a.dY) + row * a.lddy, *z = static_cast<const T *>(a.Z) + row * a.ldz;
     T *gout = static_cast<T *>(a.G) + row * a.ldg;
-    float sum = 0.f;
+    LongSum total;
     const int first = group * kActGroup, last = a.row_groups > 1 ? min(first + kActGroup, a.N) : a.N;
     for (int n0 = first + (shared ? wave * PART : 0); n0 < last; n0 += 4 * PART) {
         const int col = n0 + lane * E;
@@ -67,14 +84,16 @@ __global__ __launch_bounds__(256) void act_grad_kernel(ActGradArgs a) {
                 }
             }
         }
+        float part = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             // (a slope of 0 of ReLU and clamp stops what comes, whatever it is)
             const float s = slope(a, to_f32(zz[e])), d = to_f32(y[e]);
             const float v = a.act == kActClamp ? (s != 0.f ? d : 0.f) : d * s;
-            sum += v;
+            part += v;
             o[e] = from_f32<T>(v);
         }
+        total.add(part);
         if (col + E <= a.N) {
             __builtin_memcpy(gout + col, o, 16);
         } else {
@@ -84,6 +103,7 @@ __global__ __launch_bounds__(256) void act_grad_kernel(ActGradArgs a) {
         }
     }
     if (a.dbias == nullptr) return;
+    float sum = total.value();
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
     if (!shared) {
@@ -103,9 +123,9 @@ __global__ __launch_bounds__(256) void act_grad_kernel(ActGradArgs a) {
 __global__ __launch_bounds__(256) void row_sum_kernel(ActGradArgs a) {
     const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (row >= a.M) return;
-    float s = 0.f;
-    for (int p = 0; p < a.row_groups; ++p) s += a.part[row * a.row_groups + p];
-    a.dbias[row] = s;
+    LongSum total;
+    for (int p = 0; p < a.row_groups; ++p) total.add(a.part[row * a.row_groups + p]);
+    a.dbias[row] = total.value();
 }
 
 template <typename T> ubp_status act_grad(ActGradArgs a, hipStream_t st) {
