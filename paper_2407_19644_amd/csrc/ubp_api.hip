@@ -320,15 +320,6 @@ bool rows_overlap(const void *a, int64_t lda, const void *b, int64_t ldb, int64_
     return apart < row || pitch - apart < row;
 }
 
-// One launch through the kernels with the plain or with the wide epilogue; a preparation goes through both.
-template <class Plain, class Wide, class... A>
-ubp_status launch_either(Plain plain, Wide wide, const Epilogue &ep, bool dry, const A &...a) {
-    if (!dry) return ep.on == 2 ? wide(a..., dry) : plain(a..., dry);
-    const ubp_status rc = plain(a..., dry);
-    if (rc == UBP_OK) (void)wide(a..., dry);
-    return rc;
-}
-
 // The whole of ubp_spmm_plan / ubp_spmm_prepare / ubp_linear.  dry: everything but the launch.
 ubp_status execute(const ubp_packed *p, const void *X_dev, int64_t ldx, int32_t N, void *Y_dev, int64_t ldy, ubp_dtype y_dtype,
                    void *stream, const ubp_plan *plan, bool dry, ubp_plan *chosen, const ubp_linear_epilogue *fused) try {

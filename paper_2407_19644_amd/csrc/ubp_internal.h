@@ -560,5 +560,13 @@ ubp_status launch_blk_wide(const BlkArgs &a, bool bf16, bool y_f32, int G, int w
 ubp_status launch_xstat_wide(const TileArgs &a, bool bf16, bool y_f32, int CT, int KT, int waves, void *stream, bool dry);
 ubp_status launch_direct_wide(const DirectArgs &a, bool bf16, bool y_f32, int CT, int waves, void *stream, bool dry);
 ubp_status launch_mtile_wide(const TileArgs &a, bool bf16, bool y_f32, int shape, int rows, void *stream, bool dry);
+// One launch through the kernels with the plain or with the wide epilogue; a preparation goes through both, and fails where
+// either does (the first call would, perhaps inside a capture).
+template <class Plain, class Wide, class... A>
+ubp_status launch_either(Plain plain, Wide wide, const Epilogue &ep, bool dry, const A &...a) {
+    if (!dry) return ep.on == 2 ? wide(a..., dry) : plain(a..., dry);
+    const ubp_status rc = plain(a..., dry);
+    return rc != UBP_OK ? rc : wide(a..., dry);
+}
 
 } // namespace ubp
