@@ -71,8 +71,9 @@ __device__ __forceinline__ float sigmoid(float u) {
     return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * -1.44269504089f));
 }
 // Phi(v) = 1/2 erfc(-v / sqrt 2).  The tail Q(z) = 1 - Phi(z), z >= 0, is exp(-z^2 / 2) times a smooth function, here a
-// polynomial in t = 1 / (1 + 0.3 z): fitted for the smallest largest relative error on 0 <= z <= 14.5, where Q leaves
-// fp32, 5e-8; in fp32 Phi is within 2e-7 of the truth and its tail within 1.4e-6 of itself up to z = 5 (the rounding of z^2).
+// polynomial in t = 1 / (1 + 0.3 z): fitted for a small largest relative error on 0 <= z <= 14.5, where Q leaves fp32; with the
+// constants in fp32 it is 1e-7.  In fp32, with an exp2 and a reciprocal rounded to nearest, Phi is within 2.1e-7 of the truth, and
+// its tail within 1.5e-6 of itself up to z = 5 and 5.3e-6 up to z = 10 (the rounding of z^2).
 // density: exp(-v^2 / 2), which the slope needs too.
 __device__ __forceinline__ float normal_cdf(float v, float &density) {
     const float z = fabsf(v), t = __builtin_amdgcn_rcpf(fmaf(0.3f, z, 1.f));
