@@ -378,8 +378,8 @@ def linear(packed, X_ptr, ldx, N, Y_ptr, ldy, y_dtype, bias_ptr=None, activation
 
 def _workspace(name, packed, N):
     n = int(getattr(load_library(), name)(packed.handle, N))
-    if n < 0:
-        raise UBPError(1, name)
+    if n < 0:                       # no such size: an invalid argument, or more tokens or values than the calls take
+        raise UBPError(1 if N < 0 else 4, name)
     return n
 
 
