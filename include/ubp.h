@@ -275,7 +275,9 @@ ubp_status ubp_linear(const ubp_packed *p, const void *X_dev, int64_t ldx, int32
  * synchronisation; nothing is written on an error that a call returns before its launch.  A workspace is the caller's, 16-byte
  * aligned, of at least the bytes that the function beside the call returns for this N (0: NULL will do); what it
  * holds matters only while the call runs, and calls that may run at the same time need one each.  Results have the
- * same bits from call to call.  N above 2^31 - 2^16: UBP_ERR_UNSUPPORTED (a workspace of -1 bytes).
+ * same bits from call to call.  N above 2^31 - 2^16: UBP_ERR_UNSUPPORTED (a workspace of -1 bytes); and, for launches of 2^32
+ * threads, K ceil(N / 1024) above 2^26 - 4 for a checkpoint, M above 2^24 - 1 for ubp_linear_grad (2^26 - 4 where N is at most
+ * 256, in 16 bits 512).
  */
 
 /*
