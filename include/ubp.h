@@ -284,8 +284,9 @@ ubp_status ubp_linear(const ubp_packed *p, const void *X_dev, int64_t ldx, int32
  * G = dY act'(Z) in the handle's type and dbias[i] = sum_n of the fp32 values of G[i][n] before they are rounded.
  *   dY_dev, Z_dev, G_dev : M x N of the handle's type.  G may be dY or Z itself (the same pointer and pitch); no other overlap.
  *   activation           : UBP_ACT_*, lo and hi as in ubp_linear.  ReLU's slope is 1 above 0, clamp's from lo to hi, both
- *                          ends included; a slope of 0 gives G = 0 whatever dY is, and Z = NaN has slope 0.  UBP_ACT_NONE
- *                          copies dY and does not read Z (NULL will do).  With the others NaN stays NaN.
+ *                          ends included; with these two a slope of 0 gives G = 0 whatever dY is, and Z = NaN has slope 0.
+ *                          UBP_ACT_NONE copies dY and does not read Z (NULL will do).  With the others a NaN in Z or dY is
+ *                          one in G.
  *   dbias_dev            : M floats, overwritten, or NULL.
  * N == 0: dbias becomes 0.  UBP_ERR_INVALID_ARG: null pointer, N < 0, pitch < N, lo > hi, workspace, host-only handle.
  */

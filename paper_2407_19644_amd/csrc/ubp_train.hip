@@ -49,9 +49,9 @@ struct LongSum {
 // G's fp32 values, before they are rounded.  Four wavefronts of a workgroup take a row each, or, where rows are longer than a
 // part, every fourth part of one row (of kActGroup tokens of it, where rows are few), whose sums meet in LDS in order.  A lane's
 // sums of its 16 bytes are added up by LongSum, however many they are.
-// What bounds it: memory.  4096 rows of 8192 bf16 tokens, SiLU: 44 us, 4.58 TB/s (a large copy: 4.92).  One load of each matrix
+// What bounds it: memory.  4096 rows of 8192 bf16 tokens, SiLU: 43 us, 4.70 TB/s (a large copy: 4.92).  One load of each matrix
 // in flight per lane leaves room for 8 wavefronts per SIMD; four, with 5 wavefronts, took 54 us.  960 rows of 1568 fp16 tokens:
-// 7.9 us, the launch.
+// 7.4 us, the launch.
 template <typename T>
 __global__ __launch_bounds__(256) void act_grad_kernel(ActGradArgs a) {
     constexpr int E = 16 / (int)sizeof(T), PART = 64 * E;

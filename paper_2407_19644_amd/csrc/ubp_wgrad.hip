@@ -102,7 +102,7 @@ __device__ __forceinline__ void store_tile(const GradArgs &a, float4v sum, int s
 // Measured: 4096 x 4096, 10 % in 16 x 16 blocks, bf16, 8192 tokens from a checkpoint: 107 us with the second kernel's 9 (inputs in
 // rotation), 256 TFLOP/s of kept products; 256 x 2304, 25 % in 4 x 4 blocks, 12544 tokens: 38 us.  What bounds it: the stages'
 // parts, one behind the other.  Of the first: 11 us before and after the stages, 27 for the way into LDS and its barriers, 42 for
-// the products (LDS has 28 % of its cycles taken), 12 in which loads are waited for; loads by themselves take 40.  Two stages in
+// the products (LDS has 31 % of its cycles taken), 12 in which loads are waited for; loads by themselves take 40.  Two stages in
 // LDS, which would overlap them, leave room for half the rows: regions are smaller and read rows more often (143 us, and 41).
 template <typename T, bool CKPT, bool FAR, int TILES, int GS, int XS>
 __global__ __launch_bounds__(kThreads) void weight_grad_kernel(GradArgs a) {
