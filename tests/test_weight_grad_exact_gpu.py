@@ -104,3 +104,77 @@ def test_weight_grad_has_the_same_bits_at_every_pitch(case, dtype):
     for dv in out[1:]:
         assert torch.equal(dv, out[0])
     p.free()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("N", [31, 200, 20001])
+def test_a_checkpoint_keeps_not_finite_values_in_their_columns(N, dtype):
+    """An Inf or NaN in X is a NaN in the checkpoint, and in the weights' gradients of its own column alone."""
+    M, K = 64, 96
+    blocks = select_blocks(M, K, 8, 8, 0.4, seed=5)
+    cols = torch.from_numpy(value_cells(blocks, 8, 8)[1]).cuda()
+    p = handle(M, K, dtype, blocks, 8, 8)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(N)
+    t, G32 = _T[dtype], (N + 31) // 32
+    g, x = (torch.randn(r, N, generator=gen, device=DEV).to(t) for r in (M, K))
+    x[11, N - 1], x[40, 0], x[95, N // 2] = float("nan"), float("inf"), float("-inf")
+    q, s = torch.zeros((K, N), dtype=torch.uint8, device=DEV), torch.zeros((K, G32), dtype=torch.uint8, device=DEV)
+    n = ubp.weight_grad_workspace(p, N)
+    ws, wp = workspace(n)
+    ubp.checkpoint_save(p, x.data_ptr(), N, N, q.data_ptr(), N, s.data_ptr(), G32, stream())
+    out = []
+    for clean in (False, True):
+        if clean:                                                          # (the group's other values do not depend on them)
+            q[11, N - 1] = q[40, 0] = q[95, N // 2] = 0
+        dv = torch.full((cols.numel(),), 3.0, device=DEV)
+        ubp.weight_grad_checkpoint(p, g.data_ptr(), N, q.data_ptr(), N, s.data_ptr(), G32, N, dv.data_ptr(), False, wp, n, stream())
+        torch.cuda.synchronize()
+        out.append(dv)
+    touched = (cols == 11) | (cols == 40) | (cols == 95)
+    assert touched.any() and torch.isnan(out[0][touched]).all()
+    assert torch.equal(out[0][~touched], out[1][~touched]) and torch.isfinite(out[1]).all()
+    p.free()
+
+
+def test_calls_of_two_launches_are_captured_and_replayed():
+    """Sums over many tokens take a second launch: the bias's gradient of few rows, and the weights', added to what is there."""
+    M, K, N, dtype = 40, 64, 20001, "bf16"
+    blocks = select_blocks(M, K, 4, 4, 0.4, seed=5)
+    nv, G32 = blocks.shape[0] * 16, (N + 31) // 32
+    p = handle(M, K, dtype, blocks, 4, 4)
+    t = _T[dtype]
+    new = lambda *shape, d=t: torch.zeros(shape, dtype=d, device=DEV)      # noqa: E731
+    X, dY, Z, G = new(K, N), new(M, N), new(M, N), new(M, N)
+    Q, S = new(K, N, d=torch.uint8), new(K, G32, d=torch.uint8)
+    n, m = ubp.weight_grad_workspace(p, N), ubp.linear_grad_workspace(p, N)
+    assert n > 0 and m > 0
+    wn, wm = new(n, d=torch.uint8), new(m, d=torch.uint8)
+    ubp.weight_grad_prepare(p)
+
+    def step(db, dv):
+        st = stream()
+        ubp.checkpoint_save(p, X.data_ptr(), N, N, Q.data_ptr(), N, S.data_ptr(), G32, st)
+        ubp.linear_grad(p, dY.data_ptr(), N, Z.data_ptr(), N, N, G.data_ptr(), N, db.data_ptr(), "gelu", workspace_ptr=wm.data_ptr(),
+                        workspace_bytes=m, stream=st)
+        ubp.weight_grad_checkpoint(p, G.data_ptr(), N, Q.data_ptr(), N, S.data_ptr(), G32, N, dv.data_ptr(), False, wn.data_ptr(), n, st)
+        ubp.weight_grad(p, G.data_ptr(), N, X.data_ptr(), N, N, dv.data_ptr(), True, wn.data_ptr(), n, st)
+
+    db, dv = new(M, d=torch.float32), new(nv, d=torch.float32)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(db, dv)
+    for seed in range(3):
+        torch.manual_seed(seed)
+        for a in (X, dY, Z):
+            a.copy_(torch.randn_like(a))
+        wn.fill_(0xA5)
+        wm.fill_(0xA5)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = new(M, d=torch.float32), new(nv, d=torch.float32)
+        step(*eager)
+        torch.cuda.synchronize()
+        assert torch.equal(db, eager[0]) and torch.equal(dv, eager[1]) and dv.abs().max() > 0 and torch.isfinite(dv).all()
+    p.free()
